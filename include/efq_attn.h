@@ -302,6 +302,109 @@ int efq_pgen_bench(int kind, efq_params p, int waves, int iters, uint32_t *check
  * call. */
 int efq_clock_probe(int blocks, int iters, uint64_t *out, efq_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Positions and a paged key/value cache: rotary positions, the append of new
+ * keys and values to the cache, and softmax attention of the newest tokens of
+ * every sequence over it.  Tokens of all sequences lie one behind another
+ * (no padding between them); metadata (positions, lengths, page table) is read
+ * on the device, so no call waits for it, and a captured call takes what the
+ * buffers hold when it is replayed.
+ * ------------------------------------------------------------------------- */
+
+/* [tokens][heads][head_dim] with strides in elements between tokens and heads
+ * (a slice of a fused projection); the last dimension is contiguous.  data is
+ * 16-byte aligned, and so are both strides (in bytes). */
+typedef struct efq_rows {
+    void *data;
+    int64_t token, head;
+} efq_rows;
+
+enum efq_dtype { EFQ_BF16 = 0, EFQ_F32 = 1 };
+
+/* Rotary positions with one or several axes (time, height, width).  Pair i of
+ * a head, i < pairs, turns by pos[axis[i]][t] * inv_freq[i] for token t (the
+ * angle is formed in fp64): (x, y) -> (x cos - y sin, y cos + x sin).  Pair i
+ * is values (i, i + pairs), or (2i, 2i + 1) with interleaved; values from
+ * 2 * pairs on stay as they are.  axis NULL: every pair turns by axis 0; an
+ * entry outside [0, axes) turns its pair by nothing.  All arrays are on the
+ * device. */
+typedef struct efq_rotary {
+    int pairs, axes, interleaved;
+    const float *inv_freq;      /* [pairs]                                    */
+    const int32_t *axis;        /* [pairs] or NULL                            */
+    const int32_t *pos;         /* [axes][tokens of the call]                 */
+} efq_rotary;
+
+/* y = x with its positions applied; inverse != 0 turns back, which is the
+ * gradient: dx from dy.  y may be x (in place); other overlaps are not
+ * supported.  head_dim a multiple of 16 up to 512, pairs a multiple of 8.
+ * tokens == 0 does nothing. */
+int efq_rope(const efq_rows *x, const efq_rows *y, int tokens, int heads, int head_dim, int dtype,
+             const efq_rotary *rot, int inverse, efq_stream_t stream);
+
+/* A paged cache: pages of page_size tokens (16, 32, 64, 128 or 256), in each
+ * page one run of rows per key/value head.  head_dim is 64 or 128.
+ *   EFQ_CACHE_BF16   k, v [pages][heads_kv][page_size][head_dim] bf16
+ *   EFQ_CACHE_MXFP8  k, v [pages][heads_kv][page_size][head_dim] E4M3 bytes,
+ *                    k_scale, v_scale [..][head_dim/32] E8M0 bytes; the rule
+ *                    is that of efq_quant_qk_mxfp8, for keys and values, along
+ *                    head_dim, so an appended token changes no other.
+ * k and v are 16-byte aligned, the scales 4-byte. */
+enum efq_cache_format { EFQ_CACHE_BF16 = 0, EFQ_CACHE_MXFP8 = 1 };
+typedef struct efq_cache {
+    int pages, page_size, heads_kv, head_dim, format;
+    void *k, *v, *k_scale, *v_scale;
+} efq_cache;
+
+/* The tokens of one step.  Sequence i has seq_k[i] keys, these included; its
+ * newest ones are the tokens q_start[i] .. q_start[i + 1] - 1 of the call, in
+ * order.  Key t of sequence i lies in slot t % page_size of page
+ * page_table[i][t / page_size].  Tokens from q_start[seqs] on are padding:
+ * they are not appended, and their outputs stay as they were.
+ * tokens: rows of the call's tensors.  max_q, max_k: the largest number of new
+ * tokens and of keys of a sequence as far as the host knows (0: unknown); they
+ * choose how the work is split, and never change what is computed.
+ * Values out of range do no harm: a page outside [0, pages) holds nothing
+ * (nothing is written there, and its keys are not seen), lengths are cut to
+ * the page table's width, starts to the call's tokens; a token before its
+ * sequence's first key (more new tokens than keys) is not appended. */
+typedef struct efq_batch {
+    int seqs, tokens, table_width, max_q, max_k;
+    const int32_t *q_start;     /* [seqs + 1], rising from 0                  */
+    const int32_t *seq_k;       /* [seqs]                                     */
+    const int32_t *page_table;  /* [seqs][table_width]                        */
+} efq_batch;
+
+/* Appends: k and v (bf16, [tokens][heads_kv][head_dim]) into the cache, k with
+ * its positions applied when rot is given (pairs <= head_dim / 2; head_dim as
+ * the cache's).  The turned key is rounded to bf16, as efq_rope would, before
+ * MXFP8 rounds it further.  With q (and heads_q > 0) its rows are turned too,
+ * into q_out (which may be q): without rot that is a copy.  q NULL: keys and
+ * values only.  If two tokens fall on one slot, what it holds is unspecified;
+ * the new keys' pages must not be shared. */
+int efq_kv_append(const efq_rows *k, const efq_rows *v, const efq_cache *cache, const efq_batch *batch,
+                  const efq_rotary *rot, const efq_rows *q, int heads_q, const efq_rows *q_out,
+                  efq_stream_t stream);
+
+/* out = softmax(scale q K^T + M) V over the keys of each token's sequence.
+ * causal != 0: a token sees the keys up to its own (token j of n new ones of a
+ * sequence with s keys sees s - n + j + 1); otherwise all s.  q bf16
+ * [tokens][heads_q][head_dim], heads_q a multiple of heads_kv; out likewise,
+ * out_dtype EFQ_BF16 or EFQ_F32.  lse (fp32 [tokens][heads_q], may be NULL)
+ * receives log sum exp of the scaled scores.  A token that sees no key gets 0
+ * and -inf.  Scores, sums and accumulators are fp32, the exponential is not
+ * quantised; the probabilities enter the second product in bf16, relative
+ * to the row's maximum.  What the cache holds outside the sequences (unused
+ * slots and pages) may be anything; seen keys and values must be finite.
+ * Work is split over the keys where the rows alone do not fill the chip, which
+ * takes scratch memory: ws of efq_attn_paged_workspace_bytes (0 where nothing
+ * is split), 16-byte aligned; without it (NULL, 0) or with less, the call runs
+ * unsplit. */
+size_t efq_attn_paged_workspace_bytes(const efq_cache *cache, const efq_batch *batch, int heads_q);
+int efq_attn_paged(const efq_rows *q, int heads_q, const efq_cache *cache, const efq_batch *batch,
+                   float scale, int causal, const efq_rows *out, int out_dtype, float *lse, void *ws,
+                   size_t ws_bytes, efq_stream_t stream);
+
 const char *efq_strerror(int status);
 
 /* ABI version of this header. */

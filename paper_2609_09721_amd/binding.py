@@ -1,7 +1,7 @@
 """ctypes binding of libefq_attn.so (argument marshalling only).
 
-Every computation runs in the HIP kernels of ``csrc/efq_attn.hip``; torch
-provides device memory and the current stream.  The functions mirror the C
+Every computation runs in the HIP kernels of ``csrc/efq_attn.hip`` and
+``csrc/efq_paged.hip``; torch provides device memory and the current stream.  The functions mirror the C
 entry points of ``include/efq_attn.h``.  If the library is missing this
 module raises: there is no fallback path.
 """
@@ -44,12 +44,34 @@ class Params(ctypes.Structure):
     _fields_ = [("tau", ctypes.c_float), ("h", ctypes.c_float)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int), ("axes", ctypes.c_int), ("interleaved", ctypes.c_int),
+                ("inv_freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("pos", ctypes.c_void_p)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_int), ("page_size", ctypes.c_int), ("heads_kv", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("format", ctypes.c_int), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class Batch(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int), ("tokens", ctypes.c_int), ("table_width", ctypes.c_int),
+                ("max_q", ctypes.c_int), ("max_k", ctypes.c_int), ("q_start", ctypes.c_void_p),
+                ("seq_k", ctypes.c_void_p), ("page_table", ctypes.c_void_p)]
+
+
 _lib = None
 P = ctypes.c_void_p
 SZ = ctypes.c_size_t
 I = ctypes.c_int
 F = ctypes.c_float
 SP = ctypes.POINTER(Shape)
+RP, TP, CP, BP = (ctypes.POINTER(t) for t in (Rows, Rotary, Cache, Batch))
 
 SIGNATURES = {
     "efq_abi_version": ([], I),
@@ -81,6 +103,10 @@ SIGNATURES = {
     "efq_attn_fwd_qk8_dump": ([P, SZ, P, SZ, P, SZ, F, I, I, Params, P, SP, P, P, P, P, P], I),
     "efq_attn_lowbit_workspace_bytes": ([SP], SZ),
     "efq_attn_fwd_lowbit_ex": ([P, P, P, F, I, I, Params, P, SP, P, SZ, P], I),
+    "efq_rope": ([RP, RP, I, I, I, I, TP, I, P], I),
+    "efq_kv_append": ([RP, RP, CP, BP, TP, RP, I, RP, P], I),
+    "efq_attn_paged_workspace_bytes": ([CP, BP, I], SZ),
+    "efq_attn_paged": ([RP, I, CP, BP, F, I, RP, I, P, P, SZ, P], I),
 }
 
 
@@ -420,6 +446,216 @@ def calibrate(q, k, v, o_ref, taus, hs, scale: Optional[float] = None, causal: b
                                rho.ctypes.data_as(ctypes.c_void_p), ctypes.byref(best),
                                ctypes.c_void_p(ws.data_ptr() + off), nbytes, _stream(stream)))
     return (best.tau, best.h), rho
+
+
+# ---------------------------------------------------------------- positions, paged cache
+BF16, F32 = 0, 1
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+CACHE_BF16, CACHE_MXFP8 = 0, 1
+
+
+def _rows(t: torch.Tensor, name: str, dtype, heads=None, head_dim=None, tokens=None) -> Rows:
+    """A [tokens, heads, head_dim] tensor with any token and head strides."""
+    if t.dtype != dtype or not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{name} must be a {str(dtype)[6:]} CUDA tensor [tokens, heads, head_dim], dense in the last")
+    if (heads is not None and t.shape[1] != heads) or (head_dim is not None and t.shape[2] != head_dim) or (
+            tokens is not None and t.shape[0] != tokens):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(tokens, heads, head_dim)}")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
+    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _ints(t: torch.Tensor, name: str, shape, device) -> int:
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _rotary(pos, inv_freq, axis, interleaved, tokens: int, device) -> Rotary:
+    if pos.dim() == 1:
+        pos = pos[None]
+    if pos.dim() != 2:
+        raise ValueError("pos must be [tokens] or [axes, tokens]")
+    if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or inv_freq.device != device or inv_freq.dim() != 1:
+        raise ValueError(f"inv_freq must be a contiguous 1-D fp32 tensor on {device}")
+    if axis is None and pos.shape[0] != 1:
+        raise ValueError("several axes of positions need axis, the axis of every frequency")
+    at = _ints(pos, "pos", (pos.shape[0], tokens), device)
+    ax = None if axis is None else _ints(axis, "axis", inv_freq.shape, device)
+    return Rotary(inv_freq.shape[0], pos.shape[0], int(interleaved), inv_freq.data_ptr(), ax, at)
+
+
+def _tokens(t: torch.Tensor) -> torch.Tensor:
+    """[B, S, H, D] as [B * S, H, D], without a copy."""
+    if t.dim() != 4:
+        return t
+    B, S = t.shape[:2]
+    if B > 1 and S > 1 and t.stride(0) != S * t.stride(1):
+        raise ValueError("the batch and sequence dimensions do not merge without a copy")
+    return t.as_strided((B * S, *t.shape[2:]), (t.stride(1) if S > 1 else t.stride(0), *t.stride()[2:]))
+
+
+def rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, axis: Optional[torch.Tensor] = None,
+         interleaved: bool = False, out: Optional[torch.Tensor] = None, stream=None, _inverse: int = 0):
+    """Rotary positions: x (bf16 or fp32, [tokens, heads, head_dim] or [batch,
+    sequence, heads, head_dim], any token and head strides) with pair i of every
+    head turned by pos[axis[i], token] * inv_freq[i].
+
+    pos: int32 [axes, tokens] (or [tokens]); inv_freq: fp32 [pairs]; axis: int32
+    [pairs], None with one axis.  interleaved: pairs of neighbours instead of
+    halves.  Values behind 2 * pairs pass.  out may be x."""
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if x.dtype not in _DTYPES:
+        raise ValueError("x must be bf16 or fp32")
+    if out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
+    xs, ys = _tokens(x), _tokens(out)
+    xr, yr = _rows(xs, "x", x.dtype), _rows(ys, "out", x.dtype)
+    T, H, D = xs.shape
+    rot = _rotary(pos, inv_freq, axis, interleaved, T, x.device)
+    _check(lib().efq_rope(xr, yr, T, H, D, _DTYPES[x.dtype], rot, _inverse, _stream(stream)))
+    return out
+
+
+def rope_bwd(grad, pos, inv_freq, axis=None, interleaved=False, out=None, stream=None):
+    """The gradient of rope's x from that of its output: turned back."""
+    return rope(grad, pos, inv_freq, axis, interleaved, out, stream, _inverse=1)
+
+
+class PagedCache:
+    """Key and value pages [pages, heads_kv, page_size, head_dim]: bf16, or
+    MXFP8 as uint8 codes with uint8 scales [..., head_dim / 32]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None):
+        low = k_scale is not None
+        if (v_scale is not None) != low:
+            raise ValueError("k_scale and v_scale come together")
+        dtype = torch.uint8 if low else torch.bfloat16
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("k and v must be [pages, heads_kv, page_size, head_dim]")
+        scale_shape = (*k.shape[:3], k.shape[3] // 32)
+        for t, name, d, shape in ((k, "k", dtype, k.shape), (v, "v", dtype, k.shape), (k_scale, "k_scale", dtype, scale_shape),
+                                  (v_scale, "v_scale", dtype, scale_shape)):
+            if t is not None and (t.dtype != d or not t.is_cuda or t.device != k.device or not t.is_contiguous() or
+                                  tuple(t.shape) != tuple(shape)):
+                raise ValueError(f"{name} must be a contiguous {str(d)[6:]} CUDA tensor {tuple(shape)} on {k.device}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.pages, self.heads_kv, self.page_size, self.head_dim = k.shape
+        self.device = k.device
+        self.c = Cache(self.pages, self.page_size, self.heads_kv, self.head_dim, CACHE_MXFP8 if low else CACHE_BF16,
+                       k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if low else None,
+                       v_scale.data_ptr() if low else None)
+
+    @classmethod
+    def empty(cls, pages: int, page_size: int, heads_kv: int, head_dim: int, fmt: str = "bf16", device="cuda"):
+        """Pages that hold nothing yet; fmt: "bf16" or "mxfp8"."""
+        if fmt not in ("bf16", "mxfp8"):
+            raise ValueError(f"unknown cache format {fmt!r}")
+        shape = (pages, heads_kv, page_size, head_dim)
+        if fmt == "bf16":
+            return cls(*(torch.empty(shape, dtype=torch.bfloat16, device=device) for _ in range(2)))
+        return cls(*(torch.empty(s, dtype=torch.uint8, device=device)
+                     for s in (shape, shape, (*shape[:3], head_dim // 32), (*shape[:3], head_dim // 32))))
+
+
+class PagedBatch:
+    """The tokens of one step, for every layer of it: sequence i has seq_k[i]
+    keys, the newest being the tokens q_start[i] .. q_start[i + 1] - 1, in the
+    pages page_table[i] (int32 tensors on the GPU, read by the kernels).
+    max_q, max_k: the most new tokens and keys of a sequence, where the host
+    knows them; they choose how the work is split."""
+
+    def __init__(self, q_start: torch.Tensor, seq_k: torch.Tensor, page_table: torch.Tensor, max_q: Optional[int] = None,
+                 max_k: Optional[int] = None):
+        if seq_k.dim() != 1 or not seq_k.is_cuda or page_table.dim() != 2:
+            raise ValueError("seq_k must be a [sequences] CUDA tensor, page_table [sequences, width]")
+        n = seq_k.shape[0]
+        self.q_start, self.seq_k, self.page_table, self.device = q_start, seq_k, page_table, seq_k.device
+        self.c = (n, page_table.shape[1], int(max_q or 0), int(max_k or 0), _ints(q_start, "q_start", (n + 1,), self.device),
+                  _ints(seq_k, "seq_k", (n,), self.device),
+                  _ints(page_table, "page_table", (n, page_table.shape[1]), self.device))
+
+    def of(self, tokens: int) -> Batch:
+        n, width, q, k, a, b, c = self.c
+        return Batch(n, tokens, width, q, k, a, b, c)
+
+
+def _together(cache: PagedCache, batch: PagedBatch):
+    if cache.device != batch.device:
+        raise ValueError(f"the cache is on {cache.device}, the batch on {batch.device}")
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the call runs on cuda:{torch.cuda.current_device()}")
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, batch: PagedBatch, q: Optional[torch.Tensor] = None,
+              q_out: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+              inv_freq: Optional[torch.Tensor] = None, axis: Optional[torch.Tensor] = None, interleaved: bool = False,
+              stream=None) -> Optional[torch.Tensor]:
+    """New keys and values (bf16 [tokens, heads_kv, head_dim], any strides) into
+    the cache's pages, the keys with their positions applied when pos and
+    inv_freq are given (as in rope).  With q its rows are turned too, into q_out
+    (new when None; may be q), which is returned."""
+    _together(cache, batch)
+    T = k.shape[0]
+    kr = _rows(k, "k", torch.bfloat16, cache.heads_kv, cache.head_dim)
+    vr = _rows(v, "v", torch.bfloat16, cache.heads_kv, cache.head_dim, T)
+    if (pos is None) != (inv_freq is None):
+        raise ValueError("pos and inv_freq come together")
+    rot = None if pos is None else _rotary(pos, inv_freq, axis, interleaved, T, cache.device)
+    qr = orow = None
+    heads = 0
+    if q is not None:
+        qr = _rows(q, "q", torch.bfloat16, None, cache.head_dim, T)
+        heads = q.shape[1]
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        orow = _rows(q_out, "q_out", torch.bfloat16, heads, cache.head_dim, T)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _check(lib().efq_kv_append(kr, vr, cache.c, batch.of(T), rot, qr, heads, orow, _stream(stream)))
+    return q_out
+
+
+def attn_paged_workspace_bytes(cache: PagedCache, batch: PagedBatch, tokens: int, heads_q: int) -> int:
+    return int(lib().efq_attn_paged_workspace_bytes(cache.c, batch.of(tokens), heads_q))
+
+
+def attn_paged(q: torch.Tensor, cache: PagedCache, batch: PagedBatch, scale: Optional[float] = None, causal: bool = True,
+               out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Softmax attention of the new tokens q (bf16 [tokens, heads_q, head_dim],
+    any strides) over the pages of their sequences; a token sees the keys up to
+    its own (causal) or all.  out: bf16 or fp32 of q's shape (fp32 when None);
+    lse: fp32 [tokens, heads_q] receives the log-sum-exp.  Padding tokens keep
+    what out and lse held."""
+    _together(cache, batch)
+    qr = _rows(q, "q", torch.bfloat16, None, cache.head_dim)
+    T, H, D = q.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+    if out.dtype not in _DTYPES:
+        raise ValueError("out must be bf16 or fp32")
+    orow = _rows(out, "out", out.dtype, H, D, T)
+    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device or
+                            tuple(lse.shape) != (T, H)):
+        raise ValueError("lse must be a contiguous fp32 tensor [tokens, heads_q] on q's device")
+    b = batch.of(T)
+    if workspace is None:
+        n = int(lib().efq_attn_paged_workspace_bytes(cache.c, b, H))
+        try:
+            workspace = _scratch(n, stream)
+        except torch.OutOfMemoryError:      # without scratch the call runs unsplit
+            workspace = None
+    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.device != q.device:
+        raise ValueError("workspace must be a contiguous CUDA tensor on q's device")
+    n = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().efq_attn_paged(qr, H, cache.c, b, D ** -0.5 if scale is None else float(scale), int(causal), orow,
+                                _DTYPES[out.dtype], _ptr(lse), _ptr(workspace), n, _stream(stream)))
+    return out
+
 
 def pgen(x: torch.Tensor, kind="efq", params=None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """P-gen unit on shifted scores x [rows, cols] fp32 (CUDA)."""

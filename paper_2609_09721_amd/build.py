@@ -8,7 +8,8 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = os.path.join(PKG, "csrc", "efq_attn.hip")
+# the one translation unit: efq_paged.hip, which includes efq_attn.hip
+SRC = os.path.join(PKG, "csrc", "efq_paged.hip")
 INC = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libefq_attn.so")
 # diagnostic build of the same source with phase stamps (EFQ_PHASE_STAMPS=1);

@@ -1,0 +1,1223 @@
+// Rotary positions, a paged key/value cache and softmax attention over it, for
+// AMD Instinct MI355X (gfx950, CDNA4).
+//
+// Kernels:
+//   rope_kernel        rotary positions with one or several axes (HBM bound).
+//   kv_append_kernel   new keys (turned on the way) and values into the pages,
+//                      bf16 or MXFP8 (HBM bound; latency for a few tokens).
+//   paged_step_kernel  attention of one or a few tokens per sequence: every wave
+//                      streams keys and values of its own (HBM bound).
+//   paged_chunk_kernel attention of many tokens per sequence: waves of 32 rows
+//                      share key/value tiles in LDS (matrix-core bound).
+//   paged_merge_kernel joins the parts of a row that ran split over its keys.
+//
+// This file is the library's one translation unit: it takes the attention
+// forward, its quantisers and the host helpers in from efq_attn.hip.
+#include "efq_attn.hip"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// Round two fp32 to a pair of bf16, to nearest even (v_cvt_pk_bf16_f32).
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+  const f32x2 x = {lo, hi};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(x, bf16x2));
+}
+__device__ __forceinline__ float bf16_lo(unsigned u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
+
+// fp32 2^(byte - 127) of an E8M0 byte, as the conversions take it (0 stands
+// for 2^-127 there).
+__device__ __forceinline__ float e8m0_scale(unsigned byte) { return __uint_as_float(byte << 23); }
+
+// Four E4M3 codes times their scale as bf16, exact (4 significant bits).
+__device__ __forceinline__ uint2 e4m3_bf16x4(unsigned codes, float scale) {
+  return make_uint2(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false)),
+                    __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true)));
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Lanes l, l + 16, l + 32, l + 48 of a wave: the largest, the sum.
+__device__ __forceinline__ float max_of_groups(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmax_swapped(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmax_swapped(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_of_groups(float x) {
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// Lanes l and l + 32.
+__device__ __forceinline__ float max_of_halves(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmax_swapped(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// ------------------------------------------------------- rotary positions
+// (x, y) -> (x cos a - y sin a, y cos a + x sin a), a = pos * inv_freq.  The
+// angle's turns are formed in fp64, since fp32 would lose all of the angle's
+// fraction at far positions (a position of 2^20 leaves it 4 bits after the
+// point); the rest of a turn, in [-1/2, 1/2], goes on in fp32.  One sine and
+// cosine per token and pair serve every head: a workgroup forms them once, in
+// LDS, so the passes over the heads are loads, six operations a pair and stores.
+struct RotArgs {
+  const float* inv_freq;
+  const int32_t* axis;
+  const int32_t* pos;
+  long tokens;      // distance between the axes of pos
+  int pairs, axes, interleaved;
+};
+
+__device__ __forceinline__ float2 rot_of(const RotArgs& r, long token, int pair, bool inverse) {
+  const int ax = r.axis ? r.axis[pair] : 0;
+  const int pos = (unsigned)ax < (unsigned)r.axes ? r.pos[ax * r.tokens + token] : 0;
+  const double turns = (double)pos * (double)r.inv_freq[pair] * 0.15915494309189533577;
+  const float half = (float)(2.0 * (turns - rint(turns)));
+  float s, c;
+  sincospif(half, &s, &c);
+  return make_float2(c, inverse ? -s : s);
+}
+
+struct RopeArgs {
+  const char* x;
+  char* y;
+  long x_token, x_head, y_token, y_head;   // bytes
+  int tokens, heads, chunks;               // chunks of 16 values of a head
+  int tt;                                  // tokens of a workgroup
+  int inverse;
+  RotArgs rot;
+};
+
+// Sixteen values of a head, as fp32: 8 at lo and 8 at hi (bytes).
+template <bool F32>
+__device__ __forceinline__ void load16(const char* lo, const char* hi, float* v) {
+  if constexpr (F32) {
+    const f32x4 a = *(const f32x4*)lo, b = *(const f32x4*)(lo + 16);
+    const f32x4 c = *(const f32x4*)hi, d = *(const f32x4*)(hi + 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i], v[8 + i] = c[i], v[12 + i] = d[i];
+  } else {
+    const u32x4 a = *(const u32x4*)lo, b = *(const u32x4*)hi;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[2 * i] = bf16_lo(a[i]), v[2 * i + 1] = bf16_hi(a[i]), v[8 + 2 * i] = bf16_lo(b[i]), v[9 + 2 * i] = bf16_hi(b[i]);
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void store16(char* lo, char* hi, const float* v) {
+  if constexpr (F32) {
+    *(f32x4*)lo = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4*)(lo + 16) = f32x4{v[4], v[5], v[6], v[7]};
+    *(f32x4*)hi = f32x4{v[8], v[9], v[10], v[11]};
+    *(f32x4*)(hi + 16) = f32x4{v[12], v[13], v[14], v[15]};
+  } else {
+    u32x4 a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = pack_bf16(v[2 * i], v[2 * i + 1]), b[i] = pack_bf16(v[8 + 2 * i], v[9 + 2 * i]);
+    *(u32x4*)lo = a;
+    *(u32x4*)hi = b;
+  }
+}
+
+constexpr int kRopeTokens = 8;     // most tokens of a workgroup
+constexpr int kRopePairs = 256;    // most pairs of a head
+
+// A thread turns 8 pairs of one head: pairs 8 c .. 8 c + 7 of chunk c, each of
+// its values read once.  Chunks behind the pairs pass through.
+template <bool F32, bool INTERLEAVED>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+  extern __shared__ float2 rot[];          // [tt][pairs]
+  const long t0 = (long)blockIdx.x * a.tt;
+  const int nt = (int)min((long)a.tt, a.tokens - t0);
+  const int pairs = a.rot.pairs;
+  for (int i = threadIdx.x; i < nt * pairs; i += 256)
+    rot[i] = rot_of(a.rot, t0 + i / pairs, i % pairs, a.inverse);
+  __syncthreads();
+  constexpr int ES = F32 ? 4 : 2;
+  const int per = a.heads * a.chunks, turned = pairs / 8;
+  const int part = gridDim.y;
+  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * per; i += 256 * part) {
+    const int t = i / per, r = i % per, h = r / a.chunks, c = r % a.chunks;
+    const char* x = a.x + (t0 + t) * a.x_token + h * a.x_head;
+    char* y = a.y + (t0 + t) * a.y_token + h * a.y_head;
+    const bool turn = c < turned;
+    const bool half = !INTERLEAVED && turn;
+    const int lo = (half ? 8 * c : 16 * c) * ES, hi = (half ? pairs + 8 * c : 16 * c + 8) * ES;
+    float v[16];
+    load16<F32>(x + lo, x + hi, v);
+    if (turn) {
+      const float2* cs = rot + t * pairs + 8 * c;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int p = INTERLEAVED ? 2 * j : j, q = INTERLEAVED ? 2 * j + 1 : 8 + j;
+        const float u = v[p], w = v[q], co = cs[j].x, si = cs[j].y;
+        v[p] = __builtin_fmaf(u, co, -(w * si));
+        v[q] = __builtin_fmaf(w, co, u * si);
+      }
+    }
+    store16<F32>(y + lo, y + hi, v);
+  }
+}
+
+// ------------------------------------------------------------ paged batch
+constexpr int kMostKeys = 1 << 30;         // of a sequence: key indexes stay in 32 bits
+constexpr int kMostTokens = 1 << 26;       // of a call: launches stay within 2^32 threads
+struct Batch {
+  const int32_t *q_start, *seq_k, *table;
+  int seqs, tokens, width, pages, shift;   // page_size = 1 << shift
+  __device__ __forceinline__ int start(int i) const { return min(max(q_start[i], 0), tokens); }
+  __device__ __forceinline__ int keys(int i) const {
+    return (int)min((long)max(seq_k[i], 0), min((long)width << shift, (long)kMostKeys));
+  }
+};
+
+// The last i in [0, n) with at(i) <= x, -1 for none; at rises.  A wave looks
+// at 64 entries at a time: one load and a ballot for up to 64 sequences.
+template <typename F>
+__device__ __forceinline__ int last_at_most(int n, long x, F&& at) {
+  int found = -1;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    const int i = i0 + ((int)threadIdx.x & 63);
+    const unsigned long long b = __builtin_amdgcn_ballot_w64(i < n && at(min(i, n - 1)) <= x);
+    if (b) found = i0 + 63 - __builtin_clzll(b);
+    if (b != ~0ull) break;
+  }
+  return uniform(found);
+}
+
+// ----------------------------------------------------------------- append
+struct AppendArgs {
+  const char *k, *v, *q;
+  char *qo, *kc, *vc;
+  uint8_t *ks, *vs;
+  long k_token, k_head, v_token, v_head, q_token, q_head, o_token, o_head;   // bytes
+  Batch b;
+  int heads, heads_q, tt, rotate;
+  RotArgs rot;
+};
+
+// Eight consecutive values of a turned row: value j of chunk c, with its
+// partner from `other` (the other half of the pair, or the value beside it).
+__device__ __forceinline__ void turn8(float* v, const char* row, int c, const RotArgs& r, const float2* cs) {
+  const int pairs = r.pairs;
+  if (8 * c >= 2 * pairs) return;
+  if (r.interleaved) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 z = cs[4 * c + j];
+      const float u = v[2 * j], w = v[2 * j + 1];
+      v[2 * j] = __builtin_fmaf(u, z.x, -(w * z.y));
+      v[2 * j + 1] = __builtin_fmaf(w, z.x, u * z.y);
+    }
+    return;
+  }
+  const bool low = 8 * c < pairs;
+  const u32x4 o = *(const u32x4*)(row + 2 * (low ? 8 * c + pairs : 8 * c - pairs));
+  const float2* z = cs + (low ? 8 * c : 8 * c - pairs);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float w = (j & 1) ? bf16_hi(o[j / 2]) : bf16_lo(o[j / 2]);
+    v[j] = low ? __builtin_fmaf(v[j], z[j].x, -(w * z[j].y)) : __builtin_fmaf(v[j], z[j].x, w * z[j].y);
+  }
+}
+
+// One thread holds 8 consecutive values of a row, D / 8 threads a row, so a
+// 32-value block of MXFP8 is four neighbouring lanes, as in mxfp8_block.  A
+// turned row takes its pairs' other halves from L1.  In place (q_out = q) a
+// row's loads all precede its stores: the row belongs to one instruction of
+// one wave.
+template <int D, bool F8>
+__global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
+  extern __shared__ float2 rot[];          // [tt][pairs]
+  __shared__ long slot[kRopeTokens];       // row of head 0 in the cache, -1: none
+  constexpr int C = D / 8;
+  const long t0 = (long)blockIdx.x * a.tt;
+  const int nt = (int)min((long)a.tt, a.b.tokens - t0);
+  const int wave = threadIdx.x >> 6;
+  for (int t = wave; t < nt; t += 4) {
+    const int tok = (int)t0 + t;
+    const int i = last_at_most(a.b.seqs, tok, [&](int j) { return (long)a.b.start(j); });
+    long s = -2;                           // padding: nothing of the token is written
+    if (i >= 0 && tok < a.b.start(i + 1)) {
+      s = -1;
+      const long at = (long)a.b.keys(i) - a.b.start(i + 1) + tok;
+      if (at >= 0) {
+        const int page = a.b.table[(long)i * a.b.width + (at >> a.b.shift)];
+        if ((unsigned)page < (unsigned)a.b.pages)
+          s = (((long)page * a.heads) << a.b.shift) + (at & ((1 << a.b.shift) - 1));
+      }
+    }
+    if ((threadIdx.x & 63) == 0) slot[t] = s;
+  }
+  const int pairs = a.rotate ? a.rot.pairs : 0;
+  for (int i = threadIdx.x; i < nt * pairs; i += 256)
+    rot[i] = rot_of(a.rot, t0 + i / pairs, i % pairs, false);
+  __syncthreads();
+  const int rows = 2 * a.heads + a.heads_q;
+  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * rows * C; i += 256 * gridDim.y) {
+    const int t = i / (rows * C), r = i % (rows * C) / C, c = i % C;
+    const long s = slot[t];
+    const bool is_q = r >= 2 * a.heads, is_v = !is_q && r >= a.heads;
+    if (is_q ? s == -2 : s < 0) continue;  // whole rows
+    const int h = is_q ? r - 2 * a.heads : is_v ? r - a.heads : r;
+    const char* row = is_q ? a.q + (t0 + t) * a.q_token + h * a.q_head
+                    : is_v ? a.v + (t0 + t) * a.v_token + h * a.v_head
+                           : a.k + (t0 + t) * a.k_token + h * a.k_head;
+    u32x4 w = *(const u32x4*)(row + 16 * c);
+    if (!is_v && pairs) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[2 * j] = bf16_lo(w[j]), v[2 * j + 1] = bf16_hi(w[j]);
+      turn8(v, row, c, a.rot, rot + t * pairs);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+    }
+    if (is_q) {
+      *(u32x4*)(a.qo + (t0 + t) * a.o_token + h * a.o_head + 16 * c) = w;
+      continue;
+    }
+    const long to = s + ((long)h << a.b.shift);
+    if constexpr (!F8) {
+      *(u32x4*)((is_v ? a.vc : a.kc) + to * (2 * D) + 16 * c) = w;
+    } else {
+      unsigned am = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) am = max(am, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+      am = max(am, (unsigned)__shfl_xor((int)am, 1));
+      am = max(am, (unsigned)__shfl_xor((int)am, 2));
+      const int e = (int)(am >> 7), k = e == 0 ? -127 : max(e - 135, -127);
+      typedef __attribute__((ext_vector_type(2))) short s16x2;
+      auto y = [&](float f) { return __builtin_amdgcn_fmed3f(ldexpf(f, -k), -448.0f, 448.0f); };
+      unsigned p[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        s16x2 z = {0, 0};
+        z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(w[2 * j])), y(bf16_hi(w[2 * j])), 1.0f, false);
+        z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(w[2 * j + 1])), y(bf16_hi(w[2 * j + 1])), 1.0f, true);
+        p[j] = __builtin_bit_cast(unsigned, z);
+      }
+      *(uint2*)((is_v ? a.vc : a.kc) + to * D + 8 * c) = make_uint2(p[0], p[1]);
+      if ((c & 3) == 0) (is_v ? a.vs : a.ks)[to * (D / 32) + c / 4] = (uint8_t)(k + 127);
+    }
+  }
+}
+
+// -------------------------------------------------------- paged attention
+// Rows: the new tokens of one sequence times the G query heads that share a
+// key/value head, row r = token r / G, head h G + r % G.  A workgroup takes
+// BM of them ("slot"): slot n of the call belongs to the last sequence i with
+// floor(q_start[i] G / BM) + i <= n, so that a sequence has at least
+// ceil(new G / BM) slots whatever the lengths, and the grid, which the host
+// knows without reading them, is floor(tokens G / BM) + seqs; slots without
+// rows leave at once.
+//
+// Both kernels compute scores transposed, S^T = K Q^T, so a lane owns one row
+// (column of the product), and O^T += V^T P^T with P^T taken from the score
+// registers as they lie: the keys of a matrix instruction may come in any
+// order if both operands have the same one.  V^T comes out of row-major LDS by
+// the transposing read (ds_read_b64_tr_b16: 16 lanes give 4 rows x 16 columns,
+// each gets one column's 4 values).  The running maximum is kept in log2 units
+// (score scale log2 e), in which alpha and the probabilities are one fma and
+// one exp2; the row sum is that of the fp32 probabilities, the product takes
+// them rounded to bf16 (half a step, 2^-9 of each, independent).
+struct PagedArgs {
+  const char* q;
+  char* out;
+  float* lse;
+  const char *kc, *vc;
+  const uint8_t *ks, *vs;
+  long q_token, q_head, o_token, o_head;   // bytes
+  Batch b;
+  float sl2;                               // scale log2 e
+  int Hq, Hkv, G, causal, out_f32;
+  int nsplit, chunk;                       // most splits of a row, keys of one
+  long rows;                               // tokens * Hq
+  float* part_o;                           // [nsplit][rows][D]
+  float2* part_ml;                         // [nsplit][rows]: maximum (log2 units), sum
+};
+
+struct Slot {
+  int seq, row0, rows, q0, new_, keys;     // first row, rows of the slot; first token, new tokens, keys
+};
+
+template <int BM>
+__device__ __forceinline__ bool find_slot(const PagedArgs& a, int n, Slot& s) {
+  auto first = [&](int i) { return (long)a.b.start(i) * a.G / BM + i; };
+  s.seq = last_at_most(a.b.seqs, n, first);
+  if (s.seq < 0) return false;
+  s.q0 = a.b.start(s.seq);
+  s.new_ = max(a.b.start(s.seq + 1) - s.q0, 0);
+  s.row0 = (int)(n - first(s.seq)) * BM;
+  s.rows = min(BM, s.new_ * a.G - s.row0);
+  s.keys = a.b.keys(s.seq);
+  return s.rows > 0;
+}
+
+// Keys that row r of the slot sees.
+__device__ __forceinline__ int seen(const PagedArgs& a, const Slot& s, int r) {
+  return a.causal ? max(s.keys - s.new_ + (s.row0 + r) / a.G + 1, 0) : s.keys;
+}
+
+__device__ __forceinline__ int splits_of(const PagedArgs& a, int keys) {
+  return max(1, min(a.nsplit, (int)(((long)keys + a.chunk - 1) / a.chunk)));
+}
+
+// Final values of four consecutive columns.
+__device__ __forceinline__ void put4(char* at, int f32, f32x4 o) {
+  if (f32) *(f32x4*)at = o;
+  else *(uint2*)at = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
+}
+
+// ---- one or a few tokens
+// Four waves of a workgroup take every fourth 32-key tile of a split's keys,
+// each with its own running maximum, sum and O^T, joined at the end through
+// LDS.  Nothing is shared while streaming, so there is no barrier in the loop;
+// a wave has one tile (16 KB of bf16, D 128) on its way while it works on the
+// one before.  16 RT rows: K in matrix-operand order straight into registers,
+// V through LDS for its transposition.
+constexpr int kStepWaves = 4;
+constexpr int kStepKeys = 32;
+
+template <int D, bool F8, int RT>
+struct StepLds {
+  static constexpr int kV = kStepKeys * D * 2;                       // V tile of a wave
+  static constexpr int kO = 16 * RT * (D + 4) * 4;                   // O of a wave
+  static constexpr int kWave = kV > kO ? kV : kO;
+  static constexpr int kTotal = kStepWaves * (kWave + 16 * RT * 8);  // and maximum, sum
+};
+
+// Where chunk c (8 columns) of V row r lies: a 16-lane group reads 4 rows x 32
+// bytes, two groups 8 rows, which the swizzle spreads over all banks.
+template <int D>
+__device__ __forceinline__ int step_v_at(int r, int c) {
+  const int f = D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1;
+  return r * (2 * D) + ((c ^ f) << 4);
+}
+
+template <int D, bool F8>
+struct StepTile {
+  static constexpr int KS = D / 32;                  // k-steps of 32 columns
+  static constexpr int KN = F8 ? (D == 128 ? 2 : 1) : KS;   // 16-byte loads of a K row's lane
+  static constexpr int VN = F8 ? D / 32 : D / 16;    // 16-byte loads of V a lane
+  u32x4 k[2][KN], v[VN];
+  unsigned ksc[F8 ? 2 : 1], vsc[F8 ? VN : 1];
+  __device__ __forceinline__ void load_k(const PagedArgs& a, const long* row, int lane) {
+    const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      if constexpr (F8) {
+        const char* p = a.kc + row[hf] * D;
+        const unsigned off = r * D + g * (D / 4);
+#pragma unroll
+        for (int n = 0; n < KN; ++n) k[hf][n] = *(const u32x4*)(p + (off + 16 * n));
+        ksc[hf] = (a.ks + row[hf] * (D / 32))[(unsigned)(r * (D / 32) + g * (D / 4) / 32)];
+      } else {
+        const char* p = a.kc + row[hf] * (2 * D);
+        const unsigned off = r * (2 * D) + 16 * g;
+#pragma unroll
+        for (int n = 0; n < KN; ++n) k[hf][n] = *(const u32x4*)(p + (off + 64 * n));
+      }
+    }
+  }
+  static constexpr int VROWS = F8 ? 1024 / D : 512 / D;   // V rows of one load
+  __device__ __forceinline__ void load_v(const PagedArgs& a, const long* row, int lane) {
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      const int hf = n * VROWS / 16;
+      const unsigned r = n * VROWS % 16 + lane * VROWS / 64;
+      const unsigned c = lane % (64 / VROWS);
+      if constexpr (F8) {
+        v[n] = *(const u32x4*)(a.vc + row[hf] * D + (r * D + 16 * c));
+        vsc[n] = (a.vs + row[hf] * (D / 32))[r * (D / 32) + c / 2];
+      } else {
+        v[n] = *(const u32x4*)(a.vc + row[hf] * (2 * D) + (r * (2 * D) + 16 * c));
+      }
+    }
+  }
+  // K operand of 16-key half hf and k-step s
+  __device__ __forceinline__ bf16x8 k_op(int hf, int s) const {
+    if constexpr (F8) {
+      const float sc = e8m0_scale(ksc[hf]);
+      const uint2 x = e4m3_bf16x4(k[hf][s / 2][2 * (s & 1)], sc), y = e4m3_bf16x4(k[hf][s / 2][2 * (s & 1) + 1], sc);
+      return __builtin_bit_cast(bf16x8, u32x4{x.x, x.y, y.x, y.y});
+    } else {
+      return __builtin_bit_cast(bf16x8, k[hf][s]);
+    }
+  }
+  // rows from `live` on, and those of a page that is none, become zero
+  __device__ __forceinline__ void put_v(uint8_t* lds, int lane, bool cut, int live, const bool* bad) {
+#pragma unroll
+    for (int n = 0; n < VN; ++n) {
+      const int r = n * VROWS + lane * VROWS / 64, c = lane % (64 / VROWS);
+      if (cut && (r >= live || bad[n * VROWS / 16])) v[n] = u32x4{0u, 0u, 0u, 0u};
+      if constexpr (F8) {
+        const float sc = e8m0_scale(cut && (r >= live || bad[n * VROWS / 16]) ? 0u : vsc[n]);
+        const uint2 x = e4m3_bf16x4(v[n][0], sc), y = e4m3_bf16x4(v[n][1], sc);
+        const uint2 z = e4m3_bf16x4(v[n][2], sc), w = e4m3_bf16x4(v[n][3], sc);
+        *(u32x4*)(lds + step_v_at<D>(r, 2 * c)) = u32x4{x.x, x.y, y.x, y.y};
+        *(u32x4*)(lds + step_v_at<D>(r, 2 * c + 1)) = u32x4{z.x, z.y, w.x, w.y};
+      } else {
+        *(u32x4*)(lds + step_v_at<D>(r, c)) = v[n];
+      }
+    }
+  }
+};
+
+// Column of a head that value j of lane group g and k-step s stands for.
+template <int D, bool F8>
+__device__ __forceinline__ int step_q_col(int g, int s) {
+  return F8 ? g * (D / 4) + 8 * s : 32 * s + 8 * g;
+}
+
+template <int D, bool F8, int RT>
+__global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  typedef StepLds<D, F8, RT> L;
+  constexpr int KS = D / 32, SLABS = D / 16;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int g = lane >> 4, col = lane & 15;
+  const int h = blockIdx.x % a.Hkv, sp = blockIdx.y;
+  Slot s;
+  if (!find_slot<16 * RT>(a, (int)(blockIdx.x / a.Hkv), s)) return;
+  const int ns = splits_of(a, s.keys);
+  if (sp >= ns) return;
+  const int last = min(s.keys, seen(a, s, s.rows - 1));
+  const int k0 = (int)min((long)sp * a.chunk, (long)s.keys);
+  const int k1 = max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk));
+  const int free_of_mask = min(k1, seen(a, s, 0));     // keys below are seen by every row
+
+  bf16x8 q[RT][KS];
+  int vis[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = 16 * rt + col, row = s.row0 + min(r, s.rows - 1);
+    const char* p = a.q + (long)(s.q0 + row / a.G) * a.q_token + (h * a.G + row % a.G) * a.q_head;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) q[rt][i] = *(const bf16x8*)(p + 2 * step_q_col<D, F8>(g, i));
+    vis[rt] = min(k1, seen(a, s, min(r, s.rows - 1)));
+  }
+  f32x4 o[RT][SLABS];
+  float m[RT], l[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    m[rt] = -INFINITY;
+    l[rt] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < SLABS; ++i) o[rt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+  uint8_t* vt = lds + wave * L::kWave;
+
+  // The wave's tiles begin at k0 + 32 wave + 128 it; lane 2 (it % 32) + half
+  // holds the page of that tile's half, for 32 tiles at a time.
+  const int32_t* table = a.b.table + (long)s.seq * a.b.width;
+  const int ntiles = (k1 - k0 - kStepKeys * wave + 127) >> 7;
+  auto pages_from = [&](int it) {
+    const long key = (long)k0 + kStepKeys * wave + 128L * (it + (lane >> 1)) + 16 * (lane & 1);
+    return key < k1 ? table[key >> a.b.shift] : 0;
+  };
+  const unsigned in_page = (1u << a.b.shift) - 1;
+  auto rows_of = [&](int ids, int it, long* row, bool* bad) {
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const int id = __builtin_amdgcn_readlane(ids, 2 * (it & 31) + hf);
+      const unsigned key = k0 + kStepKeys * wave + 128 * it + 16 * hf;
+      bad[hf] = (unsigned)id >= (unsigned)a.b.pages;
+      row[hf] = (((long)(bad[hf] ? 0 : id) * a.Hkv + h) << a.b.shift) + (key & in_page);
+    }
+  };
+  if (ntiles > 0) {
+    StepTile<D, F8> t;
+    int ids = pages_from(0);
+    long row[2];
+    bool bad[2];
+    rows_of(ids, 0, row, bad);
+    t.load_k(a, row, lane);
+    t.load_v(a, row, lane);
+    for (int it = 0; it < ntiles; ++it) {
+      const int key0 = k0 + kStepKeys * wave + 128 * it;
+      const bool now_bad[2] = {bad[0], bad[1]};
+      f32x4 sc[RT][2];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) sc[rt][0] = sc[rt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          const bf16x8 kop = t.k_op(hf, i);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            sc[rt][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, q[rt][i], sc[rt][hf], 0, 0, 0);
+        }
+      const bool cut = key0 + kStepKeys > k1 || now_bad[0] || now_bad[1];
+      t.put_v(vt, lane, cut, k1 - key0, now_bad);
+      if (it + 1 < ntiles) {
+        if (((it + 1) & 31) == 0) ids = pages_from(it + 1);
+        rows_of(ids, it + 1, row, bad);
+        t.load_k(a, row, lane);
+        t.load_v(a, row, lane);
+      }
+      asm volatile("" ::: "memory");       // the tile is written before it is read; LDS keeps a wave's order
+      const bool mask = cut || key0 + kStepKeys > free_of_mask;
+      bf16x8 p[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        if (mask) {
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (key0 + 16 * hf + 4 * g + j >= vis[rt] || now_bad[hf]) sc[rt][hf][j] = -INFINITY;
+        }
+        float mx = max3f(sc[rt][0][0], sc[rt][0][1], sc[rt][0][2]);
+        mx = max3f(mx, sc[rt][0][3], sc[rt][1][0]);
+        mx = max3f(mx, sc[rt][1][1], sc[rt][1][2]);
+        mx = max_of_groups(__builtin_fmaxf(mx, sc[rt][1][3])) * a.sl2;
+        if (__builtin_amdgcn_ballot_w64(mx > m[rt])) {
+          const float mn = __builtin_fmaxf(m[rt], mx);
+          const float alpha = __builtin_amdgcn_exp2f(m[rt] - (mn == -INFINITY ? 0.0f : mn));
+          m[rt] = mn;
+          l[rt] *= alpha;
+#pragma unroll
+          for (int i = 0; i < SLABS; ++i) o[rt][i] *= alpha;
+        }
+        const float ref = m[rt] == -INFINITY ? 0.0f : m[rt];
+        u32x4 w;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][j / 2][2 * (j & 1)], a.sl2, -ref));
+          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][j / 2][2 * (j & 1) + 1], a.sl2, -ref));
+          sum += e0 + e1;
+          w[j] = pack_bf16(e0, e1);
+        }
+        l[rt] += sum;
+        p[rt] = __builtin_bit_cast(bf16x8, w);
+      }
+#pragma unroll
+      for (int i = 0; i < SLABS; ++i) {
+        const int r = 4 * g + (col >> 2), c = 2 * i + ((col >> 1) & 1), b = 8 * (col & 1);
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + step_v_at<D>(r, c) + b));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + step_v_at<D>(r + 16, c) + b));
+        const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+          o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, p[rt], o[rt][i], 0, 0, 0);
+      }
+      asm volatile("" ::: "memory");
+    }
+  }
+
+  // Join the four waves: O, maximum and sum of each through LDS.
+  __syncthreads();
+  float* ow = (float*)vt;
+  float2* ml = (float2*)(lds + kStepWaves * L::kWave);    // [wave][16 RT]
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    l[rt] = sum_of_groups(l[rt]);
+    if (g == 0) ml[wave * 16 * RT + 16 * rt + col] = make_float2(m[rt], l[rt]);
+#pragma unroll
+    for (int i = 0; i < SLABS; ++i) *(f32x4*)(ow + (16 * rt + col) * (D + 4) + 16 * i + 4 * g) = o[rt][i];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < s.rows * (D / 4); i += 64 * kStepWaves) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    float M = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kStepWaves; ++w) M = __builtin_fmaxf(M, ml[w * 16 * RT + r].x);
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (M != -INFINITY)
+#pragma unroll
+      for (int w = 0; w < kStepWaves; ++w) {
+        const float2 z = ml[w * 16 * RT + r];
+        const float e = __builtin_amdgcn_exp2f(z.x - M);
+        sum += e * z.y;
+        x += e * *(const f32x4*)((const float*)(lds + w * L::kWave) + r * (D + 4) + c);
+      }
+    const int row = s.row0 + r, tok = s.q0 + row / a.G, hq = h * a.G + row % a.G;
+    const long at = (long)tok * a.Hq + hq;
+    if (ns == 1) {
+      const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+      put4(a.out + tok * a.o_token + hq * a.o_head + c * (a.out_f32 ? 4 : 2), a.out_f32, x * inv);
+      if (c == 0 && a.lse)
+        a.lse[at] = sum > 0.0f ? (M + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+    } else {
+      *(f32x4*)(a.part_o + ((long)sp * a.rows + at) * D + c) = x;
+      if (c == 0) a.part_ml[(long)sp * a.rows + at] = make_float2(M, sum);
+    }
+  }
+}
+
+// ---- many tokens
+// NW waves of 32 rows share 64-key tiles of K and V in LDS, two of each: the
+// next tile is on its way while this one is worked on, one barrier a tile.
+template <int D>
+struct ChunkLds {
+  static constexpr int kTile = kBc * D * 2;     // bytes of 64 rows of K or V
+  static constexpr int kTotal = 4 * kTile;
+};
+
+// Swizzles of 16-byte chunk c of row r.  K: 16 rows at one column chunk. V: the
+// transposing read takes 4 rows x 64 bytes in 32 lanes.
+template <int D>
+__device__ __forceinline__ int chunk_k_swz(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int chunk_v_swz(int r) { return D == 128 ? ((r & 3) << 2) ^ (r & 2) : ((r >> 1) & 1) << 2; }
+
+// One 1 KB direct-to-LDS load: lane i's 16 bytes at `from` + voff land at
+// `to` + 16 i, zeros where voff is past `bytes`.
+__device__ __forceinline__ void load_lds_1k(const char* from, int bytes, uint8_t* to, int voff) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(from, (unsigned)bytes), to, 16, voff, 0, 0, 0);
+}
+
+template <int D, bool F8, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  constexpr int BM = 32 * NW, KK = D / 16, DT = D / 32, kTile = ChunkLds<D>::kTile;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  const int h = blockIdx.x % a.Hkv, sp = blockIdx.y;
+  Slot s;
+  // the last slots see the most keys: first
+  if (!find_slot<BM>(a, (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), s)) return;
+  const int ns = splits_of(a, s.keys);
+  if (sp >= ns) return;
+  const int last = min(s.keys, seen(a, s, s.rows - 1));
+  const int k0 = (int)min((long)sp * a.chunk, (long)s.keys);
+  const int k1 = max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk));
+  const int ntiles = (k1 - k0 + kBc - 1) / kBc;
+
+  const int r0 = 32 * wave, r = r0 + col;
+  const int row = s.row0 + min(r, s.rows - 1), tok = s.q0 + row / a.G, hq = h * a.G + row % a.G;
+  bf16x8 q[KK];
+  {
+    const char* p = a.q + (long)tok * a.q_token + hq * a.q_head;
+#pragma unroll
+    for (int i = 0; i < KK; ++i) q[i] = *(const bf16x8*)(p + 32 * i + 16 * half);
+  }
+  const int vis = min(k1, seen(a, s, min(r, s.rows - 1)));
+  const int free_of_mask = min(k1, seen(a, s, min(r0, s.rows - 1)));   // keys below are seen by the wave's rows
+  f32x16 o[DT];
+#pragma unroll
+  for (int i = 0; i < DT; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  // lane 4 (tile % 16) + quarter: the page of that 16-key quarter of the tile
+  const int32_t* table = a.b.table + (long)s.seq * a.b.width;
+  auto pages_from = [&](int tile) {
+    const long key = (long)k0 + (long)kBc * (tile + (lane >> 2)) + 16 * (lane & 3);
+    return key < k1 ? table[key >> a.b.shift] : 0;
+  };
+  auto bad_of = [&](int ids) { return __builtin_amdgcn_ballot_w64((unsigned)ids >= (unsigned)a.b.pages); };
+  const unsigned in_page = (1u << a.b.shift) - 1;
+
+  constexpr int RI = 512 / D;                        // bf16 rows of a 1 KB load
+  constexpr int PER = kBc / RI / NW;                 // loads of a wave for K, and for V
+  constexpr int C8 = kBc * D / 16 / (64 * NW);       // MXFP8: 16-code pieces of a thread (0: half of them)
+  constexpr int N8 = C8 ? C8 : 1;
+  u32x4 kr[N8], vr[N8];                              // MXFP8: the next tile's codes
+  unsigned ksr[N8], vsr[N8];
+  auto fetch = [&](int tile, int ids, int buf) {
+    const int key0 = k0 + kBc * tile;
+    if constexpr (!F8) {
+#pragma unroll
+      for (int n = 0; n < PER; ++n) {
+        const int ii = wave * PER + n, rr = ii * RI;             // first row of the load
+        const int id = __builtin_amdgcn_readlane(ids, 4 * (tile & 15) + rr / 16);
+        const bool ok = (unsigned)id < (unsigned)a.b.pages;
+        const long at = ((((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)(key0 + rr) & in_page)) * (2 * D);
+        const int rows = ok ? min(max(k1 - key0 - rr, 0), RI) : 0;
+        const int rw = rr + lane * RI / 64, c = lane % (64 / RI);
+        load_lds_1k(a.kc + at, rows * 2 * D, lds + buf * kTile + ii * 1024, (rw - rr) * 2 * D + ((c ^ chunk_k_swz<D>(rw)) << 4));
+        load_lds_1k(a.vc + at, rows * 2 * D, lds + (2 + buf) * kTile + ii * 1024, (rw - rr) * 2 * D + ((c ^ chunk_v_swz<D>(rw)) << 4));
+      }
+    } else {
+#pragma unroll
+      for (int n = 0; n < N8; ++n) {
+        const int w0 = wave + n * NW;                            // 64 pieces: 1024 / D rows
+        constexpr int R8 = 1024 / D;
+        if (C8 == 0 && w0 * R8 >= kBc) break;
+        const int id = __builtin_amdgcn_readlane(ids, 4 * (tile & 15) + w0 * R8 / 16);
+        const bool ok = (unsigned)id < (unsigned)a.b.pages;
+        const int rw = w0 * R8 + lane * R8 / 64, c = lane % (64 / R8);
+        const long at = (((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)(key0 + w0 * R8) & in_page);
+        const bool live = ok && key0 + rw < k1;
+        const unsigned off = (rw - w0 * R8) * D + 16 * c, soff = (rw - w0 * R8) * (D / 32) + c / 2;
+        kr[n] = vr[n] = u32x4{0u, 0u, 0u, 0u};
+        ksr[n] = vsr[n] = 0u;
+        if (live) {
+          kr[n] = *(const u32x4*)(a.kc + at * D + off);
+          vr[n] = *(const u32x4*)(a.vc + at * D + off);
+          ksr[n] = (a.ks + at * (D / 32))[soff];
+          vsr[n] = (a.vs + at * (D / 32))[soff];
+        }
+      }
+    }
+  };
+  auto land = [&](int buf) {
+    if constexpr (F8) {
+#pragma unroll
+      for (int n = 0; n < N8; ++n) {
+        constexpr int R8 = 1024 / D;
+        const int w0 = wave + n * NW;
+        if (C8 == 0 && w0 * R8 >= kBc) break;
+        const int rw = w0 * R8 + lane * R8 / 64, c = lane % (64 / R8);
+        auto put = [&](uint8_t* tile, u32x4 x, float sc, int swz) {
+          const uint2 e = e4m3_bf16x4(x[0], sc), f = e4m3_bf16x4(x[1], sc);
+          const uint2 y = e4m3_bf16x4(x[2], sc), z = e4m3_bf16x4(x[3], sc);
+          *(u32x4*)(tile + rw * 2 * D + (((2 * c) ^ swz) << 4)) = u32x4{e.x, e.y, f.x, f.y};
+          *(u32x4*)(tile + rw * 2 * D + (((2 * c + 1) ^ swz) << 4)) = u32x4{y.x, y.y, z.x, z.y};
+        };
+        put(lds + buf * kTile, kr[n], e8m0_scale(ksr[n]), chunk_k_swz<D>(rw));
+        put(lds + (2 + buf) * kTile, vr[n], e8m0_scale(vsr[n]), chunk_v_swz<D>(rw));
+      }
+    } else {
+      wait_vmem();
+    }
+    __syncthreads();
+  };
+
+  if (ntiles > 0) {
+    int ids = pages_from(0), next = pages_from(16);
+    unsigned long long bad = bad_of(ids), next_bad = bad;
+    fetch(0, ids, 0);
+    land(0);
+    for (int j = 0; j < ntiles; ++j) {
+      const int buf = j & 1, key0 = k0 + kBc * j;
+      const unsigned now_bad = (unsigned)(bad >> (4 * (j & 15))) & 15u;
+      if (j + 1 < ntiles) {
+        if (((j + 1) & 15) == 0) {
+          ids = next;
+          bad = bad_of(ids);
+          next = pages_from(j + 17);
+        }
+        fetch(j + 1, ids, buf ^ 1);
+      }
+      const uint8_t* kt = lds + buf * kTile;
+      const uint8_t* vt = lds + (2 + buf) * kTile;
+      f32x16 sc[2];
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[w][i] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < KK; ++i) {
+          const int kr_ = 32 * w + col;
+          const bf16x8 kop = *(const bf16x8*)(kt + kr_ * 2 * D + (((2 * i + half) ^ chunk_k_swz<D>(kr_)) << 4));
+          sc[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, q[i], sc[w], 0, 0, 0);
+        }
+      }
+      if (now_bad || key0 + kBc > free_of_mask) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int kw = 32 * w + 8 * (i >> 2) + 4 * half + (i & 3);
+            if (key0 + kw >= vis || (now_bad >> (2 * w + (i >> 3)) & 1)) sc[w][i] = -INFINITY;
+          }
+      }
+      const float mx = max_of_halves(__builtin_fmaxf(max16(sc[0]), max16(sc[1]))) * a.sl2;
+      if (__builtin_amdgcn_ballot_w64(mx > m)) {
+        const float mn = __builtin_fmaxf(m, mx);
+        const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+        m = mn;
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] *= alpha;
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int w = 0; w < 2; ++w)
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+          u32x4 pw;
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[w][8 * ks + 2 * i], a.sl2, -ref));
+            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[w][8 * ks + 2 * i + 1], a.sl2, -ref));
+            sum += e0 + e1;
+            pw[i] = pack_bf16(e0, e1);
+          }
+          l += sum;
+          const bf16x8 p = __builtin_bit_cast(bf16x8, pw);
+          const int vr0 = 32 * w + 16 * ks + 4 * half + ((lane & 15) >> 2);
+#pragma unroll
+          for (int i = 0; i < DT; ++i) {
+            const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), b = 8 * (lane & 1);
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(vt + vr0 * 2 * D + ((c ^ chunk_v_swz<D>(vr0)) << 4) + b));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_s16x4*)(vt + (vr0 + 8) * 2 * D + ((c ^ chunk_v_swz<D>(vr0 + 8)) << 4) + b));
+            const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, p, o[i], 0, 0, 0);
+          }
+        }
+      land(buf ^ 1);
+    }
+  }
+  l = sum_of_halves(l);
+  if (r >= s.rows) return;
+  const long at = (long)tok * a.Hq + hq;
+  if (ns == 1) {
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    char* p = a.out + tok * a.o_token + hq * a.o_head;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 x = {o[i][4 * j] * inv, o[i][4 * j + 1] * inv, o[i][4 * j + 2] * inv, o[i][4 * j + 3] * inv};
+        put4(p + (32 * i + 8 * j + 4 * half) * (a.out_f32 ? 4 : 2), a.out_f32, x);
+      }
+    if (half == 0 && a.lse) a.lse[at] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
+  } else {
+    float* p = a.part_o + ((long)sp * a.rows + at) * D;
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(f32x4*)(p + 32 * i + 8 * j + 4 * half) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+    if (half == 0) a.part_ml[(long)sp * a.rows + at] = make_float2(m, l);
+  }
+}
+
+// One wave per row that ran split: the parts, weighted to the common maximum,
+// summed in the order of the splits.
+template <int D>
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
+  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= a.rows) return;
+  const int lane = threadIdx.x & 63;
+  const int tok = (int)(at / a.Hq), hq = (int)(at % a.Hq);
+  const int i = last_at_most(a.b.seqs, tok, [&](int j) { return (long)a.b.start(j); });
+  if (i < 0 || tok >= a.b.start(i + 1)) return;
+  const int ns = splits_of(a, a.b.keys(i));
+  if (ns == 1) return;
+  float M = -INFINITY;
+  for (int s = lane; s < ns; s += 64) M = __builtin_fmaxf(M, a.part_ml[s * a.rows + at].x);
+  M = max_of_groups(M);
+#pragma unroll
+  for (int w = 8; w > 0; w >>= 1) M = __builtin_fmaxf(M, __shfl_xor(M, w));
+  constexpr int C = D / 64;
+  float sum = 0.0f, x[C] = {};
+  for (int s = 0; s < ns; ++s) {
+    const float2 z = a.part_ml[s * a.rows + at];
+    if (z.x == -INFINITY) continue;        // that part saw no key, and wrote no sums
+    const float e = __builtin_amdgcn_exp2f(z.x - M);
+    sum += e * z.y;
+    const float* p = a.part_o + (s * a.rows + at) * D + C * lane;
+#pragma unroll
+    for (int c = 0; c < C; ++c) x[c] += e * p[c];
+  }
+  const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+  char* out = a.out + tok * a.o_token + hq * a.o_head;
+  if constexpr (C == 2) {
+    if (a.out_f32) *(f32x2*)(out + 8 * lane) = f32x2{x[0] * inv, x[1] * inv};
+    else *(unsigned*)(out + 4 * lane) = pack_bf16(x[0] * inv, x[1] * inv);
+  } else {
+    if (a.out_f32) *(float*)(out + 4 * lane) = x[0] * inv;
+    else *(__bf16*)(out + 2 * lane) = (__bf16)(x[0] * inv);
+  }
+  if (lane == 0 && a.lse) a.lse[at] = sum > 0.0f ? (M + __builtin_amdgcn_logf(sum)) * kLn2 : -INFINITY;
+}
+
+// ================================================================ host side
+int check_rows(const efq_rows* r, const char* name, int es) {
+  if (!r || !r->data) return fail(EFQ_EINVAL, "%s is NULL", name);
+  if (!aligned16(r->data)) return fail(EFQ_EINVAL, "%s must be 16-byte aligned", name);
+  const int64_t most = (int64_t)1 << 32;   // times 2^26 tokens and 4 bytes stays in 64 bits
+  if (r->token < 0 || r->head < 0 || r->token > most || r->head > most)
+    return fail(EFQ_EINVAL, "%s: strides must be in [0, 2^32]", name);
+  if (r->token * es % 16 || r->head * es % 16)
+    return fail(EFQ_EINVAL, "%s: strides must be multiples of 16 bytes", name);
+  return EFQ_OK;
+}
+// Rows that are written: no two heads or tokens may lie on each other.
+int check_out_rows(const efq_rows* r, const char* name, int es, int tokens, int heads, int head_dim) {
+  const int rc = check_rows(r, name, es);
+  if (rc) return rc;
+  if ((heads > 1 && r->head < head_dim) || (tokens > 1 && r->token < head_dim) ||
+      (heads > 1 && tokens > 1 && r->token < r->head * (heads - 1) + head_dim &&
+       r->head < r->token * (tokens - 1) + head_dim))
+    return fail(EFQ_EINVAL, "%s: rows overlap", name);
+  return EFQ_OK;
+}
+
+int check_rotary(const efq_rotary* r, int head_dim) {
+  if (!r->inv_freq || !r->pos) return fail(EFQ_EINVAL, "rotary: null pointer");
+  if (r->axes < 1) return fail(EFQ_EINVAL, "rotary: axes must be >= 1");
+  if (r->pairs < 1 || 2 * (int64_t)r->pairs > head_dim)
+    return fail(EFQ_EINVAL, "rotary: %d pairs in a head of %d", r->pairs, head_dim);
+  if (r->pairs % 8) return fail(EFQ_EUNSUPPORTED, "rotary: pairs must be a multiple of 8");
+  return EFQ_OK;
+}
+RotArgs rot_args(const efq_rotary* r, int tokens) {
+  return RotArgs{r->inv_freq, r->axis, r->pos, tokens, r->pairs, r->axes, r->interleaved != 0};
+}
+
+int check_cache(const efq_cache* c) {
+  if (!c) return fail(EFQ_EINVAL, "cache is NULL");
+  if (c->pages < 1 || c->heads_kv < 1) return fail(EFQ_EINVAL, "cache: pages and heads_kv must be >= 1");
+  if (c->head_dim != 64 && c->head_dim != 128)
+    return fail(EFQ_EUNSUPPORTED, "cache: head_dim %d unsupported (64 or 128)", c->head_dim);
+  if (c->page_size < 16 || c->page_size > 256 || (c->page_size & (c->page_size - 1)))
+    return fail(EFQ_EUNSUPPORTED, "cache: page_size %d unsupported (16, 32, 64, 128 or 256)", c->page_size);
+  if (c->format != EFQ_CACHE_BF16 && c->format != EFQ_CACHE_MXFP8)
+    return fail(EFQ_EINVAL, "cache: unknown format %d", c->format);
+  if (!c->k || !c->v || (c->format == EFQ_CACHE_MXFP8 && (!c->k_scale || !c->v_scale)))
+    return fail(EFQ_EINVAL, "cache: null pointer");
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(EFQ_EINVAL, "cache: k and v must be 16-byte aligned");
+  if (c->format == EFQ_CACHE_MXFP8 && (((uintptr_t)c->k_scale | (uintptr_t)c->v_scale) & 3))
+    return fail(EFQ_EINVAL, "cache: scales must be 4-byte aligned");
+  return EFQ_OK;
+}
+int check_batch(const efq_batch* b) {
+  if (!b) return fail(EFQ_EINVAL, "batch is NULL");
+  if (b->seqs < 1 || b->table_width < 1 || b->tokens < 0 || b->max_q < 0 || b->max_k < 0)
+    return fail(EFQ_EINVAL, "batch: seqs and table_width must be >= 1, the rest >= 0");
+  if (b->seqs > (1 << 20) || b->tokens > kMostTokens)
+    return fail(EFQ_EUNSUPPORTED, "batch: more than 2^20 sequences or 2^26 tokens");
+  if (!b->q_start || !b->seq_k || !b->page_table) return fail(EFQ_EINVAL, "batch: null pointer");
+  return EFQ_OK;
+}
+Batch batch_args(const efq_batch* b, const efq_cache* c) {
+  return Batch{b->q_start, b->seq_k, b->page_table, b->seqs, b->tokens, b->table_width, c->pages,
+               __builtin_ctz((unsigned)c->page_size)};
+}
+
+// Tokens of a workgroup and workgroups of a token in the kernels that walk
+// over tokens: few tokens are spread over the chip a workgroup per 256 threads'
+// work, many share the sines of several tokens in one workgroup.
+void token_grid(int tokens, int threads_per_token, int& tt, int& parts) {
+  tt = std::max(1, std::min(kRopeTokens, tokens / (8 * kCUs)));
+  parts = tt > 1 || tokens > 4 * kCUs ? 1 : (threads_per_token + 255) / 256;
+}
+
+// How a call's rows are cut: the kernel, its rows per workgroup, and the
+// splits over the keys with the scratch they take.
+struct PagedPlan {
+  int rt;              // 1, 2: step kernel with 16 rt rows; 0: chunk kernel
+  int bm, nsplit, chunk;
+  long slots;
+  size_t bytes;
+};
+PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
+  PagedPlan p;
+  const int G = heads_q / c->heads_kv;
+  const long most_q = b->max_q ? b->max_q : std::max<long>(1, (long)b->tokens - b->seqs + 1);
+  const long rows = most_q * G;
+  p.rt = rows <= 16 ? 1 : rows <= 64 ? 2 : 0;
+  p.bm = p.rt ? 16 * p.rt : 256;
+  p.slots = (long)b->tokens * G / p.bm + b->seqs;
+  const long keys = std::min({(long)b->table_width * c->page_size, (long)kMostKeys, b->max_k ? (long)b->max_k : (long)kMostKeys});
+  const long items = std::max<long>(1, p.slots * c->heads_kv);
+  const long want = p.rt ? 1024 : 256, least = p.rt ? 256 : 512;
+  const long n = std::max<long>(1, std::min((want + items - 1) / items, (keys + least - 1) / least));
+  p.chunk = (int)std::min<long>(0x7fffff00L, ((keys + n - 1) / n + 127) / 128 * 128);
+  p.nsplit = (int)std::max<long>(1, (keys + p.chunk - 1) / p.chunk);
+  p.bytes = p.nsplit == 1 ? 0 : round256((size_t)p.nsplit * b->tokens * heads_q * 8) +
+                                    (size_t)p.nsplit * b->tokens * heads_q * c->head_dim * 4;
+  if (p.bytes > ((size_t)512 << 20)) {
+    p.bytes = 0;
+    p.nsplit = 1;
+  }
+  if (p.nsplit == 1) p.chunk = 0x7fffff00;
+  return p;
+}
+
+// More dynamic LDS than the default limit for one kernel, raised once per
+// device (check_device has bounded the device index); ID tells kernels apart.
+template <int ID>
+hipError_t raise_lds_of(const void* kernel, int lds) {
+  static std::once_flag once[kMaxDevices];
+  static hipError_t set_err[kMaxDevices];
+  int dev = 0;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
+  std::call_once(once[dev], [=]() {
+    set_err[dev] = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  });
+  return set_err[dev];
+}
+
+template <int D, bool F8, int RT>
+hipError_t launch_step(const PagedArgs& a, dim3 grid, hipStream_t st) {
+  constexpr int lds = StepLds<D, F8, RT>::kTotal;
+  const hipError_t e = raise_lds_of<(D * 2 + F8) * 8 + RT>((const void*)paged_step_kernel<D, F8, RT>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((paged_step_kernel<D, F8, RT>), grid, dim3(64 * kStepWaves), lds, st, a);
+  return hipGetLastError();
+}
+template <int D, bool F8, int NW>
+hipError_t launch_chunk(const PagedArgs& a, dim3 grid, hipStream_t st) {
+  constexpr int lds = ChunkLds<D>::kTotal;
+  const hipError_t e = raise_lds_of<(D * 2 + F8) * 8>((const void*)paged_chunk_kernel<D, F8, NW>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((paged_chunk_kernel<D, F8, NW>), grid, dim3(64 * NW), lds, st, a);
+  return hipGetLastError();
+}
+template <int D, bool F8>
+hipError_t launch_paged(const PagedArgs& a, const PagedPlan& p, hipStream_t st) {
+  const dim3 grid((unsigned)(p.slots * a.Hkv), (unsigned)a.nsplit);
+  const hipError_t e = p.rt == 1 ? launch_step<D, F8, 1>(a, grid, st)
+                     : p.rt == 2 ? launch_step<D, F8, 2>(a, grid, st)
+                                 : launch_chunk<D, F8, 8>(a, grid, st);
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  hipLaunchKernelGGL(paged_merge_kernel<D>, dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// ================================================================== C ABI
+extern "C" {
+
+int efq_rope(const efq_rows* x, const efq_rows* y, int tokens, int heads, int head_dim, int dtype,
+             const efq_rotary* rot, int inverse, efq_stream_t stream) {
+  if (tokens < 0 || heads < 1 || head_dim < 1) return fail(EFQ_EINVAL, "tokens must be >= 0, heads and head_dim >= 1");
+  if (head_dim % 16 || head_dim > 512)
+    return fail(EFQ_EUNSUPPORTED, "head_dim %d unsupported (a multiple of 16 up to 512)", head_dim);
+  if (heads > (1 << 16) || tokens > kMostTokens)
+    return fail(EFQ_EUNSUPPORTED, "more than 2^16 heads or 2^26 tokens");
+  if (dtype != EFQ_BF16 && dtype != EFQ_F32) return fail(EFQ_EINVAL, "unknown dtype %d", dtype);
+  if (!rot) return fail(EFQ_EINVAL, "rotary is NULL");
+  if (tokens == 0) return EFQ_OK;
+  const int es = dtype == EFQ_F32 ? 4 : 2;
+  int rc;
+  if ((rc = check_rotary(rot, head_dim)) || (rc = check_rows(x, "x", es)) ||
+      (rc = check_out_rows(y, "y", es, tokens, heads, head_dim)))
+    return rc;
+  if ((rc = check_device())) return rc;
+  RopeArgs a;
+  a.x = (const char*)x->data;
+  a.y = (char*)y->data;
+  a.x_token = x->token * es, a.x_head = x->head * es, a.y_token = y->token * es, a.y_head = y->head * es;
+  a.tokens = tokens, a.heads = heads, a.chunks = head_dim / 16, a.inverse = inverse != 0;
+  a.rot = rot_args(rot, tokens);
+  int parts;
+  token_grid(tokens, heads * a.chunks, a.tt, parts);
+  const dim3 grid((unsigned)(((long)tokens + a.tt - 1) / a.tt), (unsigned)parts);
+  const int lds = a.tt * rot->pairs * (int)sizeof(float2);
+  hipStream_t st = (hipStream_t)stream;
+  if (es == 4 && rot->interleaved) hipLaunchKernelGGL((rope_kernel<true, true>), grid, dim3(256), lds, st, a);
+  else if (es == 4) hipLaunchKernelGGL((rope_kernel<true, false>), grid, dim3(256), lds, st, a);
+  else if (rot->interleaved) hipLaunchKernelGGL((rope_kernel<false, true>), grid, dim3(256), lds, st, a);
+  else hipLaunchKernelGGL((rope_kernel<false, false>), grid, dim3(256), lds, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(EFQ_EHIP, "rope launch: %s", hipGetErrorString(e));
+  return EFQ_OK;
+}
+
+int efq_kv_append(const efq_rows* k, const efq_rows* v, const efq_cache* cache, const efq_batch* batch,
+                  const efq_rotary* rot, const efq_rows* q, int heads_q, const efq_rows* q_out,
+                  efq_stream_t stream) {
+  int rc;
+  if ((rc = check_cache(cache)) || (rc = check_batch(batch))) return rc;
+  const int D = cache->head_dim;
+  if (q ? heads_q < 1 || heads_q > (1 << 16) : heads_q != 0)
+    return fail(EFQ_EINVAL, "heads_q must be in [1, 65536] with q and 0 without");
+  if (cache->heads_kv > (1 << 16)) return fail(EFQ_EUNSUPPORTED, "more than 65536 heads");
+  if (batch->tokens == 0) return EFQ_OK;
+  if ((rc = check_rows(k, "k", 2)) || (rc = check_rows(v, "v", 2))) return rc;
+  if (rot && (rc = check_rotary(rot, D))) return rc;
+  if (q && ((rc = check_rows(q, "q", 2)) || (rc = check_out_rows(q_out, "q_out", 2, batch->tokens, heads_q, D)))) return rc;
+  if ((rc = check_device())) return rc;
+  AppendArgs a;
+  memset(&a, 0, sizeof a);
+  a.k = (const char*)k->data, a.k_token = 2 * k->token, a.k_head = 2 * k->head;
+  a.v = (const char*)v->data, a.v_token = 2 * v->token, a.v_head = 2 * v->head;
+  if (q) {
+    a.q = (const char*)q->data, a.q_token = 2 * q->token, a.q_head = 2 * q->head;
+    a.qo = (char*)q_out->data, a.o_token = 2 * q_out->token, a.o_head = 2 * q_out->head;
+  }
+  a.kc = (char*)cache->k, a.vc = (char*)cache->v;
+  a.ks = (uint8_t*)cache->k_scale, a.vs = (uint8_t*)cache->v_scale;
+  a.b = batch_args(batch, cache);
+  a.heads = cache->heads_kv, a.heads_q = heads_q;
+  if (rot) a.rotate = 1, a.rot = rot_args(rot, batch->tokens);
+  int parts;
+  token_grid(batch->tokens, (2 * a.heads + heads_q) * (D / 8), a.tt, parts);
+  const dim3 grid((unsigned)(((long)batch->tokens + a.tt - 1) / a.tt), (unsigned)parts);
+  const int lds = rot ? a.tt * rot->pairs * (int)sizeof(float2) : 0;
+  hipStream_t st = (hipStream_t)stream;
+  const bool f8 = cache->format == EFQ_CACHE_MXFP8;
+  if (D == 128 && f8) hipLaunchKernelGGL((kv_append_kernel<128, true>), grid, dim3(256), lds, st, a);
+  else if (D == 128) hipLaunchKernelGGL((kv_append_kernel<128, false>), grid, dim3(256), lds, st, a);
+  else if (f8) hipLaunchKernelGGL((kv_append_kernel<64, true>), grid, dim3(256), lds, st, a);
+  else hipLaunchKernelGGL((kv_append_kernel<64, false>), grid, dim3(256), lds, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(EFQ_EHIP, "append launch: %s", hipGetErrorString(e));
+  return EFQ_OK;
+}
+
+static int check_paged(const efq_cache* cache, const efq_batch* batch, int heads_q) {
+  int rc;
+  if ((rc = check_cache(cache)) || (rc = check_batch(batch))) return rc;
+  if (heads_q < 1 || heads_q > (1 << 16) || heads_q % cache->heads_kv)
+    return fail(EFQ_EINVAL, "heads_q %d not a positive multiple of heads_kv %d (up to 65536)", heads_q, cache->heads_kv);
+  const long G = heads_q / cache->heads_kv;
+  if (((long)batch->tokens * G / 16 + batch->seqs) * cache->heads_kv >= (1L << 22) || (long)batch->tokens * heads_q >= (1L << 25))
+    return fail(EFQ_EUNSUPPORTED, "batch: too many tokens for one call");
+  return EFQ_OK;
+}
+
+size_t efq_attn_paged_workspace_bytes(const efq_cache* cache, const efq_batch* batch, int heads_q) {
+  if (check_paged(cache, batch, heads_q) != EFQ_OK || batch->tokens == 0) return 0;
+  return paged_plan(cache, batch, heads_q).bytes;
+}
+
+int efq_attn_paged(const efq_rows* q, int heads_q, const efq_cache* cache, const efq_batch* batch,
+                   float scale, int causal, const efq_rows* out, int out_dtype, float* lse, void* ws,
+                   size_t ws_bytes, efq_stream_t stream) {
+  int rc;
+  if ((rc = check_paged(cache, batch, heads_q)) || (rc = check_scale(scale))) return rc;
+  if (out_dtype != EFQ_BF16 && out_dtype != EFQ_F32) return fail(EFQ_EINVAL, "unknown dtype %d", out_dtype);
+  if (batch->tokens == 0) return EFQ_OK;
+  const int D = cache->head_dim;
+  if ((rc = check_rows(q, "q", 2)) ||
+      (rc = check_out_rows(out, "out", out_dtype == EFQ_F32 ? 4 : 2, batch->tokens, heads_q, D)))
+    return rc;
+  if ((uintptr_t)lse & 3) return fail(EFQ_EINVAL, "lse must be 4-byte aligned");
+  if (ws_bytes != 0 && !ws) return fail(EFQ_EWORKSPACE, "workspace is NULL");
+  if (ws && !aligned16(ws)) return fail(EFQ_EINVAL, "workspace must be 16-byte aligned");
+  if ((rc = check_device())) return rc;
+  PagedPlan p = paged_plan(cache, batch, heads_q);
+  PagedArgs a;
+  const int es = out_dtype == EFQ_F32 ? 4 : 2;
+  a.q = (const char*)q->data, a.q_token = 2 * q->token, a.q_head = 2 * q->head;
+  a.out = (char*)out->data, a.o_token = es * out->token, a.o_head = es * out->head;
+  a.lse = lse;
+  a.kc = (const char*)cache->k, a.vc = (const char*)cache->v;
+  a.ks = (const uint8_t*)cache->k_scale, a.vs = (const uint8_t*)cache->v_scale;
+  a.b = batch_args(batch, cache);
+  a.sl2 = scale * kInvLn2;
+  a.Hq = heads_q, a.Hkv = cache->heads_kv, a.G = heads_q / cache->heads_kv;
+  a.causal = causal != 0, a.out_f32 = out_dtype == EFQ_F32;
+  a.rows = (long)batch->tokens * heads_q;
+  if (ws_bytes < p.bytes) p.nsplit = 1, p.chunk = 0x7fffff00;
+  a.nsplit = p.nsplit, a.chunk = p.chunk;
+  a.part_ml = (float2*)ws;
+  a.part_o = (float*)((uint8_t*)ws + round256((size_t)p.nsplit * a.rows * 8));
+  hipStream_t st = (hipStream_t)stream;
+  const bool f8 = cache->format == EFQ_CACHE_MXFP8;
+  const hipError_t e = D == 128 ? (f8 ? launch_paged<128, true>(a, p, st) : launch_paged<128, false>(a, p, st))
+                                : (f8 ? launch_paged<64, true>(a, p, st) : launch_paged<64, false>(a, p, st));
+  if (e != hipSuccess) return fail(EFQ_EHIP, "paged attention launch: %s", hipGetErrorString(e));
+  return EFQ_OK;
+}
+
+}  // extern "C"
