@@ -183,16 +183,24 @@ struct Batch {
   }
 };
 
-// The last i in [0, n) with at(i) <= x, -1 for none; at rises.  A wave looks
-// at 64 entries at a time: one load and a ballot for up to 64 sequences.
+// The last sequence i with at(i, start(i)) <= x, -1 for none, where at rises;
+// first and end get start(i) and start(i + 1).  A wave looks at 64 sequences at
+// a time: two loads and a ballot for up to 64.
 template <typename F>
-__device__ __forceinline__ int last_at_most(int n, long x, F&& at) {
+__device__ __forceinline__ int last_at_most(const Batch& b, long x, F&& at, int& first, int& end) {
   int found = -1;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    const int i = i0 + ((int)threadIdx.x & 63);
-    const unsigned long long b = __builtin_amdgcn_ballot_w64(i < n && at(min(i, n - 1)) <= x);
-    if (b) found = i0 + 63 - __builtin_clzll(b);
-    if (b != ~0ull) break;
+  first = end = 0;
+  for (int i0 = 0; i0 < b.seqs; i0 += 64) {
+    const int i = i0 + ((int)threadIdx.x & 63), j = min(i, b.seqs - 1);
+    const int s = b.start(j), e = b.start(j + 1);
+    const unsigned long long m = __builtin_amdgcn_ballot_w64(i < b.seqs && at(j, s) <= x);
+    if (m) {
+      const int l = 63 - __builtin_clzll(m);
+      found = i0 + l;
+      first = __builtin_amdgcn_readlane(s, l);
+      end = __builtin_amdgcn_readlane(e, l);
+    }
+    if (m != ~0ull) break;
   }
   return uniform(found);
 }
@@ -248,11 +256,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   const int wave = threadIdx.x >> 6;
   for (int t = wave; t < nt; t += 4) {
     const int tok = (int)t0 + t;
-    const int i = last_at_most(a.b.seqs, tok, [&](int j) { return (long)a.b.start(j); });
+    int first, end;
+    const int i = last_at_most(a.b, tok, [](int, int start) { return (long)start; }, first, end);
     long s = -2;                           // padding: nothing of the token is written
-    if (i >= 0 && tok < a.b.start(i + 1)) {
+    if (i >= 0 && tok < end) {
       s = -1;
-      const long at = (long)a.b.keys(i) - a.b.start(i + 1) + tok;
+      const long at = (long)a.b.keys(i) - end + tok;
       if (at >= 0) {
         const int page = a.b.table[(long)i * a.b.width + (at >> a.b.shift)];
         if ((unsigned)page < (unsigned)a.b.pages)
@@ -331,7 +340,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // each gets one column's 4 values).  The running maximum is kept in log2 units
 // (score scale log2 e), in which alpha and the probabilities are one fma and
 // one exp2; the row sum is that of the fp32 probabilities, the product takes
-// them rounded to bf16 (half a step, 2^-9 of each, independent).
+// them rounded to bf16 (at most 2^-8 of each, independent of one another).
 struct PagedArgs {
   const char* q;
   char* out;
@@ -352,16 +361,17 @@ struct Slot {
   int seq, row0, rows, q0, new_, keys;     // first row, rows of the slot; first token, new tokens, keys
 };
 
+// The slot but for `keys`, which the caller loads beside what else it knows to
+// ask for by then.
 template <int BM>
 __device__ __forceinline__ bool find_slot(const PagedArgs& a, int n, Slot& s) {
-  auto first = [&](int i) { return (long)a.b.start(i) * a.G / BM + i; };
-  s.seq = last_at_most(a.b.seqs, n, first);
+  auto at = [&](int i, int start) { return (long)start * a.G / BM + i; };
+  int end;
+  s.seq = last_at_most(a.b, n, at, s.q0, end);
   if (s.seq < 0) return false;
-  s.q0 = a.b.start(s.seq);
-  s.new_ = max(a.b.start(s.seq + 1) - s.q0, 0);
-  s.row0 = (int)(n - first(s.seq)) * BM;
+  s.new_ = max(end - s.q0, 0);
+  s.row0 = (int)(n - at(s.seq, s.q0)) * BM;
   s.rows = min(BM, s.new_ * a.G - s.row0);
-  s.keys = a.b.keys(s.seq);
   return s.rows > 0;
 }
 
@@ -381,18 +391,18 @@ __device__ __forceinline__ void put4(char* at, int f32, f32x4 o) {
 }
 
 // ---- one or a few tokens
-// Four waves of a workgroup take every fourth 32-key tile of a split's keys,
-// each with its own running maximum, sum and O^T, joined at the end through
-// LDS.  Nothing is shared while streaming, so there is no barrier in the loop;
-// a wave has one tile (16 KB of bf16, D 128) on its way while it works on the
-// one before.  16 RT rows: K in matrix-operand order straight into registers,
-// V through LDS for its transposition.
+// Four waves of a workgroup take every fourth tile (16 kStepHalves keys) of a split's
+// keys, each with its own running maximum, sum and O^T, joined at the end
+// through LDS.  Nothing is shared while streaming, so there is no barrier in
+// the loop; a wave has one tile on its way while it works on the one before.
+// 16 RT rows: K in matrix-operand order straight into registers, V through LDS
+// for its transposition.
 constexpr int kStepWaves = 4;
-constexpr int kStepKeys = 32;
+constexpr int kStepHalves = 2;       // 16-key halves of a wave's tile
 
-template <int D, bool F8, int RT>
+template <int D, int RT>
 struct StepLds {
-  static constexpr int kV = kStepKeys * D * 2;                       // V tile of a wave
+  static constexpr int kV = 16 * kStepHalves * D * 2;                         // V tile of a wave
   static constexpr int kO = 16 * RT * (D + 4) * 4;                   // O of a wave
   static constexpr int kWave = kV > kO ? kV : kO;
   static constexpr int kTotal = kStepWaves * (kWave + 16 * RT * 8);  // and maximum, sum
@@ -406,32 +416,37 @@ __device__ __forceinline__ int step_v_at(int r, int c) {
   return r * (2 * D) + ((c ^ f) << 4);
 }
 
+// Keys and values are read once, so their loads ask the caches not to keep
+// them: one token over 131000 keys (32/8 heads, D 128, bf16) 99.9 -> 87.5 us
+// (5.37 -> 6.13 TB/s), 300 tokens over 1000 keys each 141 -> 131 us.
+__device__ __forceinline__ u32x4 stream16(const char* p) { return __builtin_nontemporal_load((const u32x4*)p); }
+
+// One tile in registers.  A lane has row lane % 16 of every 16-key half of K:
+// 16-byte pieces g, g + 4, .. of it (g = lane / 16), so that a load takes 64
+// consecutive bytes of 16 rows; V by whole rows.
 template <int D, bool F8>
 struct StepTile {
-  static constexpr int KS = D / 32;                  // k-steps of 32 columns
-  static constexpr int KN = F8 ? (D == 128 ? 2 : 1) : KS;   // 16-byte loads of a K row's lane
-  static constexpr int VN = F8 ? D / 32 : D / 16;    // 16-byte loads of V a lane
-  u32x4 k[2][KN], v[VN];
-  unsigned ksc[F8 ? 2 : 1], vsc[F8 ? VN : 1];
+  static constexpr int KS = D / 32;                       // k-steps of 32 columns
+  static constexpr int KN = F8 ? D / 64 : D / 32;         // 16-byte pieces of a K row's lane
+  static constexpr int VN = kStepHalves * (F8 ? D / 64 : D / 32);  // 16-byte pieces of V a lane
+  static constexpr int VROWS = F8 ? 1024 / D : 512 / D;   // V rows of one load
+  u32x4 k[kStepHalves][KN], v[VN];
+  unsigned ksc[F8 ? kStepHalves : 1], vsc[F8 ? VN : 1];            // a K row's scales, a V piece's scale
   __device__ __forceinline__ void load_k(const PagedArgs& a, const long* row, int lane) {
-    const int r = lane & 15, g = lane >> 4;
+    const unsigned r = lane & 15, g = lane >> 4;
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
+    for (int hf = 0; hf < kStepHalves; ++hf) {
+      const char* p = a.kc + row[hf] * (F8 ? D : 2 * D);
+      const unsigned off = r * (F8 ? D : 2 * D) + 16 * g;
+#pragma unroll
+      for (int n = 0; n < KN; ++n) k[hf][n] = stream16(p + (off + 64 * n));
       if constexpr (F8) {
-        const char* p = a.kc + row[hf] * D;
-        const unsigned off = r * D + g * (D / 4);
-#pragma unroll
-        for (int n = 0; n < KN; ++n) k[hf][n] = *(const u32x4*)(p + (off + 16 * n));
-        ksc[hf] = (a.ks + row[hf] * (D / 32))[(unsigned)(r * (D / 32) + g * (D / 4) / 32)];
-      } else {
-        const char* p = a.kc + row[hf] * (2 * D);
-        const unsigned off = r * (2 * D) + 16 * g;
-#pragma unroll
-        for (int n = 0; n < KN; ++n) k[hf][n] = *(const u32x4*)(p + (off + 64 * n));
+        const uint8_t* e = a.ks + row[hf] * (D / 32);
+        if constexpr (D == 128) ksc[hf] = *(const unsigned*)(e + 4 * r);
+        else ksc[hf] = *(const unsigned short*)(e + 2 * r);
       }
     }
   }
-  static constexpr int VROWS = F8 ? 1024 / D : 512 / D;   // V rows of one load
   __device__ __forceinline__ void load_v(const PagedArgs& a, const long* row, int lane) {
 #pragma unroll
     for (int n = 0; n < VN; ++n) {
@@ -439,17 +454,18 @@ struct StepTile {
       const unsigned r = n * VROWS % 16 + lane * VROWS / 64;
       const unsigned c = lane % (64 / VROWS);
       if constexpr (F8) {
-        v[n] = *(const u32x4*)(a.vc + row[hf] * D + (r * D + 16 * c));
+        v[n] = stream16(a.vc + row[hf] * D + (r * D + 16 * c));
         vsc[n] = (a.vs + row[hf] * (D / 32))[r * (D / 32) + c / 2];
       } else {
-        v[n] = *(const u32x4*)(a.vc + row[hf] * (2 * D) + (r * (2 * D) + 16 * c));
+        v[n] = stream16(a.vc + row[hf] * (2 * D) + (r * (2 * D) + 16 * c));
       }
     }
   }
-  // K operand of 16-key half hf and k-step s
-  __device__ __forceinline__ bf16x8 k_op(int hf, int s) const {
+  // K operand of 16-key half hf and k-step s: the columns of step_q_col
+  __device__ __forceinline__ bf16x8 k_op(int hf, int s, int g) const {
     if constexpr (F8) {
-      const float sc = e8m0_scale(ksc[hf]);
+      // piece s / 2 has codes 64 (s / 2) + 16 g ..: block 2 (s / 2) + g / 2
+      const float sc = e8m0_scale((ksc[hf] >> (16 * (s / 2) + 8 * (g >> 1))) & 255u);
       const uint2 x = e4m3_bf16x4(k[hf][s / 2][2 * (s & 1)], sc), y = e4m3_bf16x4(k[hf][s / 2][2 * (s & 1) + 1], sc);
       return __builtin_bit_cast(bf16x8, u32x4{x.x, x.y, y.x, y.y});
     } else {
@@ -457,13 +473,14 @@ struct StepTile {
     }
   }
   // rows from `live` on, and those of a page that is none, become zero
-  __device__ __forceinline__ void put_v(uint8_t* lds, int lane, bool cut, int live, const bool* bad) {
+  __device__ __forceinline__ void put_v(uint8_t* lds, int lane, bool cut, int live, unsigned bad) {
 #pragma unroll
     for (int n = 0; n < VN; ++n) {
       const int r = n * VROWS + lane * VROWS / 64, c = lane % (64 / VROWS);
-      if (cut && (r >= live || bad[n * VROWS / 16])) v[n] = u32x4{0u, 0u, 0u, 0u};
+      const bool none = cut && (r >= live || (bad >> (n * VROWS / 16) & 1));
+      if (none) v[n] = u32x4{0u, 0u, 0u, 0u};
       if constexpr (F8) {
-        const float sc = e8m0_scale(cut && (r >= live || bad[n * VROWS / 16]) ? 0u : vsc[n]);
+        const float sc = e8m0_scale(none ? 0u : vsc[n]);
         const uint2 x = e4m3_bf16x4(v[n][0], sc), y = e4m3_bf16x4(v[n][1], sc);
         const uint2 z = e4m3_bf16x4(v[n][2], sc), w = e4m3_bf16x4(v[n][3], sc);
         *(u32x4*)(lds + step_v_at<D>(r, 2 * c)) = u32x4{x.x, x.y, y.x, y.y};
@@ -475,39 +492,51 @@ struct StepTile {
   }
 };
 
-// Column of a head that value j of lane group g and k-step s stands for.
+// First of the 8 columns of a head that lane group g holds in k-step s.
 template <int D, bool F8>
 __device__ __forceinline__ int step_q_col(int g, int s) {
-  return F8 ? g * (D / 4) + 8 * s : 32 * s + 8 * g;
+  return F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
 }
 
 template <int D, bool F8, int RT>
 __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
-  typedef StepLds<D, F8, RT> L;
-  constexpr int KS = D / 32, SLABS = D / 16;
+  typedef StepLds<D, RT> L;
+  constexpr int KS = D / 32, SLABS = D / 16, KEYS = 16 * kStepHalves, ROUND = kStepWaves * KEYS, AHEAD = 64 / kStepHalves;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int g = lane >> 4, col = lane & 15;
   const int h = blockIdx.x % a.Hkv, sp = blockIdx.y;
   Slot s;
   if (!find_slot<16 * RT>(a, (int)(blockIdx.x / a.Hkv), s)) return;
-  const int ns = splits_of(a, s.keys);
-  if (sp >= ns) return;
-  const int last = min(s.keys, seen(a, s, s.rows - 1));
-  const int k0 = (int)min((long)sp * a.chunk, (long)s.keys);
-  const int k1 = max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk));
-  const int free_of_mask = min(k1, seen(a, s, 0));     // keys below are seen by every row
 
+  // The wave's tiles begin at k0 + KEYS wave + ROUND it; lane kStepHalves (it % AHEAD) +
+  // half holds the page of that tile's half, for AHEAD tiles at a time.  The
+  // first ones, and Q, are asked for beside the sequence's length.
+  const int k0 = (int)min((long)sp * a.chunk, (long)kMostKeys);
+  const int32_t* table = a.b.table + (long)s.seq * a.b.width;
+  auto pages_from = [&](int it) {
+    const long key = (long)k0 + KEYS * wave + (long)ROUND * (it + lane / kStepHalves) + 16 * (lane % kStepHalves);
+    const long at = key >> a.b.shift;
+    return at < a.b.width ? table[at] : 0;
+  };
+  int ids = pages_from(0);
   bf16x8 q[RT][KS];
-  int vis[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int r = 16 * rt + col, row = s.row0 + min(r, s.rows - 1);
+    const int row = s.row0 + min(16 * rt + col, s.rows - 1);
     const char* p = a.q + (long)(s.q0 + row / a.G) * a.q_token + (h * a.G + row % a.G) * a.q_head;
 #pragma unroll
     for (int i = 0; i < KS; ++i) q[rt][i] = *(const bf16x8*)(p + 2 * step_q_col<D, F8>(g, i));
-    vis[rt] = min(k1, seen(a, s, min(r, s.rows - 1)));
   }
+  s.keys = a.b.keys(s.seq);
+  const int ns = splits_of(a, s.keys);
+  if (sp >= ns) return;
+  const int last = min(s.keys, seen(a, s, s.rows - 1));
+  const int k1 = max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk));
+  const int free_of_mask = min(k1, seen(a, s, 0));     // keys below are seen by every row
+  int vis[RT];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) vis[rt] = min(k1, seen(a, s, min(16 * rt + col, s.rows - 1)));
   f32x4 o[RT][SLABS];
   float m[RT], l[RT];
 #pragma unroll
@@ -519,71 +548,72 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
   }
   uint8_t* vt = lds + wave * L::kWave;
 
-  // The wave's tiles begin at k0 + 32 wave + 128 it; lane 2 (it % 32) + half
-  // holds the page of that tile's half, for 32 tiles at a time.
-  const int32_t* table = a.b.table + (long)s.seq * a.b.width;
-  const int ntiles = (k1 - k0 - kStepKeys * wave + 127) >> 7;
-  auto pages_from = [&](int it) {
-    const long key = (long)k0 + kStepKeys * wave + 128L * (it + (lane >> 1)) + 16 * (lane & 1);
-    return key < k1 ? table[key >> a.b.shift] : 0;
-  };
+  const int ntiles = (k1 - k0 - KEYS * wave + ROUND - 1) / ROUND;
   const unsigned in_page = (1u << a.b.shift) - 1;
-  auto rows_of = [&](int ids, int it, long* row, bool* bad) {
+  // cache rows of a tile's halves; a bit for each half whose page is none.
+  // Halves behind the last key stay within their sequence's pages, or page 0.
+  auto rows_of = [&](int it, long* row) {
+    unsigned bad = 0;
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf) {
-      const int id = __builtin_amdgcn_readlane(ids, 2 * (it & 31) + hf);
-      const unsigned key = k0 + kStepKeys * wave + 128 * it + 16 * hf;
-      bad[hf] = (unsigned)id >= (unsigned)a.b.pages;
-      row[hf] = (((long)(bad[hf] ? 0 : id) * a.Hkv + h) << a.b.shift) + (key & in_page);
+    for (int hf = 0; hf < kStepHalves; ++hf) {
+      const int id = __builtin_amdgcn_readlane(ids, kStepHalves * (it % AHEAD) + hf);
+      const unsigned key = k0 + KEYS * wave + ROUND * it + 16 * hf;
+      const bool none = (unsigned)id >= (unsigned)a.b.pages;
+      if (none) bad |= 1u << hf;
+      row[hf] = (((long)(none ? 0 : id) * a.Hkv + h) << a.b.shift) + (key & in_page);
     }
+    return bad;
   };
   if (ntiles > 0) {
     StepTile<D, F8> t;
-    int ids = pages_from(0);
-    long row[2];
-    bool bad[2];
-    rows_of(ids, 0, row, bad);
+    long row[kStepHalves];
+    unsigned bad = rows_of(0, row);
     t.load_k(a, row, lane);
     t.load_v(a, row, lane);
     for (int it = 0; it < ntiles; ++it) {
-      const int key0 = k0 + kStepKeys * wave + 128 * it;
-      const bool now_bad[2] = {bad[0], bad[1]};
-      f32x4 sc[RT][2];
+      const int key0 = k0 + KEYS * wave + ROUND * it;
+      const unsigned now_bad = bad;
+      f32x4 sc[RT][kStepHalves];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) sc[rt][0] = sc[rt][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
+        for (int hf = 0; hf < kStepHalves; ++hf) sc[rt][hf] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int hf = 0; hf < kStepHalves; ++hf)
 #pragma unroll
         for (int i = 0; i < KS; ++i) {
-          const bf16x8 kop = t.k_op(hf, i);
+          const bf16x8 kop = t.k_op(hf, i, g);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
             sc[rt][hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop, q[rt][i], sc[rt][hf], 0, 0, 0);
         }
-      const bool cut = key0 + kStepKeys > k1 || now_bad[0] || now_bad[1];
+      const bool cut = key0 + KEYS > k1 || now_bad;
       t.put_v(vt, lane, cut, k1 - key0, now_bad);
       if (it + 1 < ntiles) {
-        if (((it + 1) & 31) == 0) ids = pages_from(it + 1);
-        rows_of(ids, it + 1, row, bad);
+        if ((it + 1) % AHEAD == 0) ids = pages_from(it + 1);
+        bad = rows_of(it + 1, row);
         t.load_k(a, row, lane);
         t.load_v(a, row, lane);
       }
       asm volatile("" ::: "memory");       // the tile is written before it is read; LDS keeps a wave's order
-      const bool mask = cut || key0 + kStepKeys > free_of_mask;
-      bf16x8 p[RT];
+      const bool mask = cut || key0 + KEYS > free_of_mask;
+      bf16x8 p[RT][kStepHalves / 2];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         if (mask) {
 #pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
+          for (int hf = 0; hf < kStepHalves; ++hf)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              if (key0 + 16 * hf + 4 * g + j >= vis[rt] || now_bad[hf]) sc[rt][hf][j] = -INFINITY;
+              if (key0 + 16 * hf + 4 * g + j >= vis[rt] || (now_bad >> hf & 1)) sc[rt][hf][j] = -INFINITY;
         }
-        float mx = max3f(sc[rt][0][0], sc[rt][0][1], sc[rt][0][2]);
-        mx = max3f(mx, sc[rt][0][3], sc[rt][1][0]);
-        mx = max3f(mx, sc[rt][1][1], sc[rt][1][2]);
-        mx = max_of_groups(__builtin_fmaxf(mx, sc[rt][1][3])) * a.sl2;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int hf = 0; hf < kStepHalves; ++hf) {
+          mx = max3f(mx, sc[rt][hf][0], sc[rt][hf][1]);
+          mx = max3f(mx, sc[rt][hf][2], sc[rt][hf][3]);
+        }
+        mx = max_of_groups(mx) * a.sl2;
         if (__builtin_amdgcn_ballot_w64(mx > m[rt])) {
           const float mn = __builtin_fmaxf(m[rt], mx);
           const float alpha = __builtin_amdgcn_exp2f(m[rt] - (mn == -INFINITY ? 0.0f : mn));
@@ -593,28 +623,34 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
           for (int i = 0; i < SLABS; ++i) o[rt][i] *= alpha;
         }
         const float ref = m[rt] == -INFINITY ? 0.0f : m[rt];
-        u32x4 w;
-        float sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][j / 2][2 * (j & 1)], a.sl2, -ref));
-          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rt][j / 2][2 * (j & 1) + 1], a.sl2, -ref));
-          sum += e0 + e1;
-          w[j] = pack_bf16(e0, e1);
+        for (int pr = 0; pr < kStepHalves / 2; ++pr) {
+          u32x4 w;
+          float sum = 0.0f;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x4& x = sc[rt][2 * pr + j / 2];
+            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * (j & 1)], a.sl2, -ref));
+            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * (j & 1) + 1], a.sl2, -ref));
+            sum += e0 + e1;
+            w[j] = pack_bf16(e0, e1);
+          }
+          l[rt] += sum;
+          p[rt][pr] = __builtin_bit_cast(bf16x8, w);
         }
-        l[rt] += sum;
-        p[rt] = __builtin_bit_cast(bf16x8, w);
       }
 #pragma unroll
-      for (int i = 0; i < SLABS; ++i) {
-        const int r = 4 * g + (col >> 2), c = 2 * i + ((col >> 1) & 1), b = 8 * (col & 1);
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + step_v_at<D>(r, c) + b));
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + step_v_at<D>(r + 16, c) + b));
-        const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      for (int pr = 0; pr < kStepHalves / 2; ++pr)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt)
-          o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, p[rt], o[rt][i], 0, 0, 0);
-      }
+        for (int i = 0; i < SLABS; ++i) {
+          const int r = 32 * pr + 4 * g + (col >> 2), c = 2 * i + ((col >> 1) & 1), b = 8 * (col & 1);
+          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + step_v_at<D>(r, c) + b));
+          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + step_v_at<D>(r + 16, c) + b));
+          const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+            o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vop, p[rt][pr], o[rt][i], 0, 0, 0);
+        }
       asm volatile("" ::: "memory");
     }
   }
@@ -691,6 +727,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   Slot s;
   // the last slots see the most keys: first
   if (!find_slot<BM>(a, (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), s)) return;
+  s.keys = a.b.keys(s.seq);
   const int ns = splits_of(a, s.keys);
   if (sp >= ns) return;
   const int last = min(s.keys, seen(a, s, s.rows - 1));
@@ -894,33 +931,64 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   }
 }
 
-// One wave per row that ran split: the parts, weighted to the common maximum,
-// summed in the order of the splits.
+// W waves (1 or 4) per row that ran split: the parts, weighted to the common
+// maximum, every W-th part by one wave, then the waves in order.  A short
+// kernel is its chain of dependent loads, so the maxima are asked for before
+// the sequence's length is known, and four parts' sums at a time.
 template <int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
-  const long at = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (at >= a.rows) return;
-  const int lane = threadIdx.x & 63;
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a, int W) {
+  constexpr int C = D / 64;
+  __shared__ float shared[4][C * 64 + 1];
+  const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const long at = W == 4 ? (long)blockIdx.x : (long)blockIdx.x * 4 + wave;
+  if (at >= a.rows) return;                  // whole workgroups where waves share a row
+  const float early = lane < a.nsplit ? a.part_ml[lane * a.rows + at].x : -INFINITY;
   const int tok = (int)(at / a.Hq), hq = (int)(at % a.Hq);
-  const int i = last_at_most(a.b.seqs, tok, [&](int j) { return (long)a.b.start(j); });
-  if (i < 0 || tok >= a.b.start(i + 1)) return;
+  int first, end;
+  const int i = last_at_most(a.b, tok, [](int, int start) { return (long)start; }, first, end);
+  if (i < 0 || tok >= end) return;
   const int ns = splits_of(a, a.b.keys(i));
   if (ns == 1) return;
-  float M = -INFINITY;
-  for (int s = lane; s < ns; s += 64) M = __builtin_fmaxf(M, a.part_ml[s * a.rows + at].x);
+  float M = lane < ns ? early : -INFINITY;
+  for (int s = lane + 64; s < ns; s += 64) M = __builtin_fmaxf(M, a.part_ml[s * a.rows + at].x);
   M = max_of_groups(M);
 #pragma unroll
   for (int w = 8; w > 0; w >>= 1) M = __builtin_fmaxf(M, __shfl_xor(M, w));
-  constexpr int C = D / 64;
+  const float ref = M == -INFINITY ? 0.0f : M;
+  const int w0 = W == 4 ? wave : 0;
   float sum = 0.0f, x[C] = {};
-  for (int s = 0; s < ns; ++s) {
-    const float2 z = a.part_ml[s * a.rows + at];
-    if (z.x == -INFINITY) continue;        // that part saw no key, and wrote no sums
-    const float e = __builtin_amdgcn_exp2f(z.x - M);
-    sum += e * z.y;
-    const float* p = a.part_o + (s * a.rows + at) * D + C * lane;
+  for (int s0 = w0; s0 < ns; s0 += 4 * W) {
+    float e[4], v[4][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) x[c] += e * p[c];
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + u * W;
+      const long from = min(s, ns - 1) * a.rows + at;
+      const float2 z = a.part_ml[from];
+      e[u] = s < ns ? __builtin_amdgcn_exp2f(z.x - ref) : 0.0f;     // 0 for a part that saw no key
+      sum += e[u] * z.y;
+#pragma unroll
+      for (int c = 0; c < C; ++c) v[u][c] = a.part_o[from * D + C * lane + c];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+#pragma unroll
+      for (int c = 0; c < C; ++c) x[c] = __builtin_fmaf(e[u], v[u][c], x[c]);
+  }
+  if (W == 4) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) shared[wave][C * lane + c] = x[c];
+    if (lane == 0) shared[wave][C * 64] = sum;
+    __syncthreads();
+    if (wave > 0) return;
+    sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) x[c] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      sum += shared[w][C * 64];
+#pragma unroll
+      for (int c = 0; c < C; ++c) x[c] += shared[w][C * lane + c];
+    }
   }
   const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
   char* out = a.out + tok * a.o_token + hq * a.o_head;
@@ -1024,9 +1092,25 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
   p.slots = (long)b->tokens * G / p.bm + b->seqs;
   const long keys = std::min({(long)b->table_width * c->page_size, (long)kMostKeys, b->max_k ? (long)b->max_k : (long)kMostKeys});
   const long items = std::max<long>(1, p.slots * c->heads_kv);
-  const long want = p.rt ? 1024 : 256, least = p.rt ? 256 : 512;
-  const long n = std::max<long>(1, std::min((want + items - 1) / items, (keys + least - 1) / least));
-  p.chunk = (int)std::min<long>(0x7fffff00L, ((keys + n - 1) / n + 127) / 128 * 128);
+  // Splits of the longest sequence.  Step kernel: as many as put two
+  // workgroups on every CU; sequences of different lengths (more than one)
+  // also want pieces small enough to end together, down to 448 KB of keys and
+  // values, which stream in about ten times what it takes to start a
+  // workgroup.  17 sequences of 5000 to 20000 keys (32/8 heads, D 128, bf16) in
+  // pieces of 6700 / 2900 / 1540 / 830 keys: 164 / 171 / 145 / 138 us; one of
+  // 131000 keys in 64 / 256 pieces 87 / 98 us.  No piece is below 512 keys: its
+  // join would cost more than it saves (one sequence of 500 keys in two 15.0
+  // us, in one 10.9).
+  long n;
+  if (p.rt) {
+    const long key_bytes = 2 * (c->format == EFQ_CACHE_BF16 ? 2 * c->head_dim : c->head_dim + c->head_dim / 32);
+    n = (2 * kCUs + items - 1) / items;
+    if (b->seqs > 1) n = std::max(n, keys * key_bytes / (448 << 10));
+  } else {
+    n = (kCUs + items - 1) / items;
+  }
+  n = std::max<long>(1, std::min(n, keys / 512));
+  p.chunk = (int)(((keys + n - 1) / n + 127) / 128 * 128);
   p.nsplit = (int)std::max<long>(1, (keys + p.chunk - 1) / p.chunk);
   p.bytes = p.nsplit == 1 ? 0 : round256((size_t)p.nsplit * b->tokens * heads_q * 8) +
                                     (size_t)p.nsplit * b->tokens * heads_q * c->head_dim * 4;
@@ -1056,7 +1140,7 @@ hipError_t raise_lds_of(const void* kernel, int lds) {
 
 template <int D, bool F8, int RT>
 hipError_t launch_step(const PagedArgs& a, dim3 grid, hipStream_t st) {
-  constexpr int lds = StepLds<D, F8, RT>::kTotal;
+  constexpr int lds = StepLds<D, RT>::kTotal;
   const hipError_t e = raise_lds_of<(D * 2 + F8) * 8 + RT>((const void*)paged_step_kernel<D, F8, RT>, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((paged_step_kernel<D, F8, RT>), grid, dim3(64 * kStepWaves), lds, st, a);
@@ -1077,7 +1161,8 @@ hipError_t launch_paged(const PagedArgs& a, const PagedPlan& p, hipStream_t st) 
                      : p.rt == 2 ? launch_step<D, F8, 2>(a, grid, st)
                                  : launch_chunk<D, F8, 8>(a, grid, st);
   if (e != hipSuccess || a.nsplit == 1) return e;
-  hipLaunchKernelGGL(paged_merge_kernel<D>, dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, st, a);
+  const int W = a.nsplit > 4 ? 4 : 1;
+  hipLaunchKernelGGL(paged_merge_kernel<D>, dim3((unsigned)(W == 4 ? a.rows : (a.rows + 3) / 4)), dim3(256), 0, st, a, W);
   return hipGetLastError();
 }
 
