@@ -454,36 +454,47 @@ _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 CACHE_BF16, CACHE_MXFP8 = 0, 1
 
 
-def _rows(t: torch.Tensor, name: str, dtype, heads=None, head_dim=None, tokens=None) -> Rows:
-    """A [tokens, heads, head_dim] tensor with any token and head strides."""
-    if t.dtype != dtype or not t.is_cuda or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
-        raise ValueError(f"{name} must be a {str(dtype)[6:]} CUDA tensor [tokens, heads, head_dim], dense in the last")
-    if (heads is not None and t.shape[1] != heads) or (head_dim is not None and t.shape[2] != head_dim) or (
-            tokens is not None and t.shape[0] != tokens):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(tokens, heads, head_dim)}")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the call runs on cuda:{torch.cuda.current_device()}")
-    return Rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+def _place(name: str, at: int, dev: int):
+    raise ValueError(f"{name} is on {'the CPU' if at < 0 else f'cuda:{at}'}, the call runs on cuda:{dev}")
 
 
-def _ints(t: torch.Tensor, name: str, shape, device) -> int:
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {device}")
+def _rows(t: torch.Tensor, name: str, dtype, dev: int, heads=None, head_dim=None, tokens=None) -> Rows:
+    """A [tokens, heads, head_dim] tensor with any token and head strides on device `dev`."""
+    shape = t.shape
+    if t.dtype is not dtype or len(shape) != 3:
+        raise ValueError(f"{name} must be a {str(dtype)[6:]} tensor [tokens, heads, head_dim]")
+    T, H, D = shape
+    if (heads is not None and H != heads) or (head_dim is not None and D != head_dim) or (tokens is not None and T != tokens):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected {(tokens, heads, head_dim)}")
+    if t.get_device() != dev:
+        _place(name, t.get_device(), dev)
+    st, sh, sd = t.stride()
+    if sd != 1 and D > 1:
+        raise ValueError(f"{name} must be dense in its last dimension")
+    return Rows(t.data_ptr(), st if T > 1 else 0, sh if H > 1 else 0)
+
+
+def _ints(t: torch.Tensor, name: str, shape: tuple, dev: int) -> int:
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)}")
+    if t.get_device() != dev:
+        _place(name, t.get_device(), dev)
     return t.data_ptr()
 
 
-def _rotary(pos, inv_freq, axis, interleaved, tokens: int, device) -> Rotary:
-    if pos.dim() == 1:
-        pos = pos[None]
-    if pos.dim() != 2:
+def _rotary(pos, inv_freq, axis, interleaved, tokens: int, dev: int) -> Rotary:
+    if pos.dim() not in (1, 2):
         raise ValueError("pos must be [tokens] or [axes, tokens]")
-    if inv_freq.dtype != torch.float32 or not inv_freq.is_contiguous() or inv_freq.device != device or inv_freq.dim() != 1:
-        raise ValueError(f"inv_freq must be a contiguous 1-D fp32 tensor on {device}")
-    if axis is None and pos.shape[0] != 1:
+    axes = 1 if pos.dim() == 1 else pos.shape[0]
+    if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        raise ValueError("inv_freq must be a contiguous 1-D fp32 tensor")
+    if inv_freq.get_device() != dev:
+        _place("inv_freq", inv_freq.get_device(), dev)
+    if axis is None and axes != 1:
         raise ValueError("several axes of positions need axis, the axis of every frequency")
-    at = _ints(pos, "pos", (pos.shape[0], tokens), device)
-    ax = None if axis is None else _ints(axis, "axis", inv_freq.shape, device)
-    return Rotary(inv_freq.shape[0], pos.shape[0], int(interleaved), inv_freq.data_ptr(), ax, at)
+    at = _ints(pos, "pos", (tokens,) if pos.dim() == 1 else (axes, tokens), dev)
+    ax = None if axis is None else _ints(axis, "axis", inv_freq.shape, dev)
+    return Rotary(inv_freq.shape[0], axes, interleaved, inv_freq.data_ptr(), ax, at)
 
 
 def _tokens(t: torch.Tensor) -> torch.Tensor:
@@ -505,17 +516,19 @@ def rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, axis: Optio
     pos: int32 [axes, tokens] (or [tokens]); inv_freq: fp32 [pairs]; axis: int32
     [pairs], None with one axis.  interleaved: pairs of neighbours instead of
     halves.  Values behind 2 * pairs pass.  out may be x."""
-    if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if x.dtype not in _DTYPES:
+    dtype = x.dtype
+    if dtype not in _DTYPES:
         raise ValueError("x must be bf16 or fp32")
-    if out.shape != x.shape:
+    if out is None:
+        out = torch.empty(x.shape, dtype=dtype, device=x.device)
+    elif out.shape != x.shape:
         raise ValueError("out must have the shape of x")
-    xs, ys = _tokens(x), _tokens(out)
-    xr, yr = _rows(xs, "x", x.dtype), _rows(ys, "out", x.dtype)
+    dev = torch.cuda.current_device()
+    xs = _tokens(x)
+    xr, yr = _rows(xs, "x", dtype, dev), _rows(_tokens(out), "out", dtype, dev)
     T, H, D = xs.shape
-    rot = _rotary(pos, inv_freq, axis, interleaved, T, x.device)
-    _check(lib().efq_rope(xr, yr, T, H, D, _DTYPES[x.dtype], rot, _inverse, _stream(stream)))
+    rot = _rotary(pos, inv_freq, axis, interleaved, T, dev)
+    _check(lib().efq_rope(xr, yr, T, H, D, _DTYPES[dtype], rot, _inverse, _stream(stream)))
     return out
 
 
@@ -544,7 +557,7 @@ class PagedCache:
                 raise ValueError(f"{name} must be a contiguous {str(d)[6:]} CUDA tensor {tuple(shape)} on {k.device}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.pages, self.heads_kv, self.page_size, self.head_dim = k.shape
-        self.device = k.device
+        self.dev = k.get_device()
         self.c = Cache(self.pages, self.page_size, self.heads_kv, self.head_dim, CACHE_MXFP8 if low else CACHE_BF16,
                        k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if low else None,
                        v_scale.data_ptr() if low else None)
@@ -572,22 +585,30 @@ class PagedBatch:
                  max_k: Optional[int] = None):
         if seq_k.dim() != 1 or not seq_k.is_cuda or page_table.dim() != 2:
             raise ValueError("seq_k must be a [sequences] CUDA tensor, page_table [sequences, width]")
-        n = seq_k.shape[0]
-        self.q_start, self.seq_k, self.page_table, self.device = q_start, seq_k, page_table, seq_k.device
-        self.c = (n, page_table.shape[1], int(max_q or 0), int(max_k or 0), _ints(q_start, "q_start", (n + 1,), self.device),
-                  _ints(seq_k, "seq_k", (n,), self.device),
-                  _ints(page_table, "page_table", (n, page_table.shape[1]), self.device))
+        n, width = page_table.shape
+        dev = seq_k.get_device()
+        self.q_start, self.seq_k, self.page_table, self.dev = q_start, seq_k, page_table, dev
+        self._fields = (width, int(max_q or 0), int(max_k or 0), _ints(q_start, "q_start", (n + 1,), dev),
+                        _ints(seq_k, "seq_k", (n,), dev), _ints(page_table, "page_table", (n, width), dev))
+        self.seqs = n
+        self._last = (-1, None)
 
     def of(self, tokens: int) -> Batch:
-        n, width, q, k, a, b, c = self.c
-        return Batch(n, tokens, width, q, k, a, b, c)
+        """The batch as the C entry points take it, with the calls' number of tokens."""
+        last = self._last
+        if last[0] != tokens:
+            self._last = last = (tokens, Batch(self.seqs, tokens, *self._fields))
+        return last[1]
 
 
-def _together(cache: PagedCache, batch: PagedBatch):
-    if cache.device != batch.device:
-        raise ValueError(f"the cache is on {cache.device}, the batch on {batch.device}")
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the call runs on cuda:{torch.cuda.current_device()}")
+def _together(cache: PagedCache, batch: PagedBatch) -> int:
+    """The device of both, which has to be the one the call runs on."""
+    dev = torch.cuda.current_device()
+    if cache.dev != dev:
+        _place("the cache", cache.dev, dev)
+    if batch.dev != dev:
+        _place("the batch", batch.dev, dev)
+    return dev
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, batch: PagedBatch, q: Optional[torch.Tensor] = None,
@@ -598,21 +619,22 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, batch: PagedB
     the cache's pages, the keys with their positions applied when pos and
     inv_freq are given (as in rope).  With q its rows are turned too, into q_out
     (new when None; may be q), which is returned."""
-    _together(cache, batch)
+    dev = _together(cache, batch)
+    bf16, H, D = torch.bfloat16, cache.heads_kv, cache.head_dim
+    kr = _rows(k, "k", bf16, dev, H, D)
     T = k.shape[0]
-    kr = _rows(k, "k", torch.bfloat16, cache.heads_kv, cache.head_dim)
-    vr = _rows(v, "v", torch.bfloat16, cache.heads_kv, cache.head_dim, T)
+    vr = _rows(v, "v", bf16, dev, H, D, T)
     if (pos is None) != (inv_freq is None):
         raise ValueError("pos and inv_freq come together")
-    rot = None if pos is None else _rotary(pos, inv_freq, axis, interleaved, T, cache.device)
+    rot = None if pos is None else _rotary(pos, inv_freq, axis, interleaved, T, dev)
     qr = orow = None
     heads = 0
     if q is not None:
-        qr = _rows(q, "q", torch.bfloat16, None, cache.head_dim, T)
+        qr = _rows(q, "q", bf16, dev, None, D, T)
         heads = q.shape[1]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        orow = _rows(q_out, "q_out", torch.bfloat16, heads, cache.head_dim, T)
+            q_out = torch.empty(q.shape, dtype=bf16, device=q.device)
+        orow = _rows(q_out, "q_out", bf16, dev, heads, D, T)
     elif q_out is not None:
         raise ValueError("q_out without q")
     _check(lib().efq_kv_append(kr, vr, cache.c, batch.of(T), rot, qr, heads, orow, _stream(stream)))
@@ -631,29 +653,32 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, batch: PagedBatch, scale: Opt
     its own (causal) or all.  out: bf16 or fp32 of q's shape (fp32 when None);
     lse: fp32 [tokens, heads_q] receives the log-sum-exp.  Padding tokens keep
     what out and lse held."""
-    _together(cache, batch)
-    qr = _rows(q, "q", torch.bfloat16, None, cache.head_dim)
+    dev = _together(cache, batch)
+    qr = _rows(q, "q", torch.bfloat16, dev, None, cache.head_dim)
     T, H, D = q.shape
     if out is None:
         out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
-    if out.dtype not in _DTYPES:
+    dtype = _DTYPES.get(out.dtype)
+    if dtype is None:
         raise ValueError("out must be bf16 or fp32")
-    orow = _rows(out, "out", out.dtype, H, D, T)
-    if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != q.device or
-                            tuple(lse.shape) != (T, H)):
+    orow = _rows(out, "out", out.dtype, dev, H, D, T)
+    if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, H) or not lse.is_contiguous() or
+                            lse.get_device() != dev):
         raise ValueError("lse must be a contiguous fp32 tensor [tokens, heads_q] on q's device")
-    b = batch.of(T)
+    b, l = batch.of(T), lib()
     if workspace is None:
-        n = int(lib().efq_attn_paged_workspace_bytes(cache.c, b, H))
-        try:
-            workspace = _scratch(n, stream)
-        except torch.OutOfMemoryError:      # without scratch the call runs unsplit
-            workspace = None
-    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.device != q.device:
+        n = l.efq_attn_paged_workspace_bytes(cache.c, b, H)
+        if n:
+            try:
+                workspace = _scratch(n, stream)
+            except torch.OutOfMemoryError:      # without scratch the call runs unsplit
+                pass
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous CUDA tensor on q's device")
     n = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().efq_attn_paged(qr, H, cache.c, b, D ** -0.5 if scale is None else float(scale), int(causal), orow,
-                                _DTYPES[out.dtype], _ptr(lse), _ptr(workspace), n, _stream(stream)))
+    _check(l.efq_attn_paged(qr, H, cache.c, b, D ** -0.5 if scale is None else float(scale), causal, orow, dtype,
+                            None if lse is None else lse.data_ptr(), None if workspace is None else workspace.data_ptr(), n,
+                            _stream(stream)))
     return out
 
 
