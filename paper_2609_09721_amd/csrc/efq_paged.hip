@@ -696,12 +696,26 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
 }
 
 // ---- many tokens
-// NW waves of 32 rows share 64-key tiles of K and V in LDS, two of each: the
-// next tile is on its way while this one is worked on, one barrier a tile.
-template <int D>
+// Waves of 32 rows share 64-key tiles of K and V in LDS, two of each.  A SIMD
+// overlaps its matrix core and its vector unit when one of its two waves does
+// only matrix work and the other only vector work, not when both do some of
+// each; so the waves form two groups that swap phases at a barrier: while one
+// group runs M (scores of tile j + 1, P V of tile j: 32 matrix instructions at
+// D 128), the other runs V (maxima and exponentials of a tile).  K runs one
+// tile ahead of V, the loads one tile ahead of both.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(std::integral_constant<int, I>{});
+    static_for<N, I + 1>(f);
+  }
+}
+
+template <int D, bool F8>
 struct ChunkLds {
   static constexpr int kTile = kBc * D * 2;     // bytes of 64 rows of K or V
-  static constexpr int kTotal = 4 * kTile;
+  static constexpr int kRing = F8 ? 3 : 4;      // tiles of each
+  static constexpr int kTotal = 2 * kRing * kTile;
 };
 
 // Swizzles of 16-byte chunk c of row r.  K: 16 rows at one column chunk. V: the
@@ -711,16 +725,106 @@ __device__ __forceinline__ int chunk_k_swz(int r) { return D == 128 ? r & 15 : (
 template <int D>
 __device__ __forceinline__ int chunk_v_swz(int r) { return D == 128 ? ((r & 3) << 2) ^ (r & 2) : ((r >> 1) & 1) << 2; }
 
-// One 1 KB direct-to-LDS load: lane i's 16 bytes at `from` + voff land at
-// `to` + 16 i, zeros where voff is past `bytes`.
-__device__ __forceinline__ void load_lds_1k(const char* from, int bytes, uint8_t* to, int voff) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(from, (unsigned)bytes), to, 16, voff, 0, 0, 0);
+// One 1 KB direct-to-LDS load: lane i's 16 bytes at `from` + voff land at LDS
+// address `to` + 16 i, zeros where voff is past `bytes`.  In assembly, since
+// the compiler would wait for all such loads before the next transposing read;
+// it has no register output, and the kernel's own waits count it.  Waits that
+// the compiler places for its loads count it too, and so only wait longer.
+__device__ __forceinline__ void load_lds_1k(const char* from, int bytes, unsigned to, int voff) {
+  const unsigned long long p = (unsigned long long)from;
+  const u32x4 rsrc = {(unsigned)p, (unsigned)(p >> 32) & 0xffffu, (unsigned)bytes, 0x00020000u};
+  // (five wait states from a vector instruction that writes a scalar register to
+  // a memory instruction that reads it, one from the write of m0, which the
+  // compiler sets anew before any instruction of its own that reads it)
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(to), "v"(voff), "s"(rsrc) : "memory");
 }
+
+// A kernel's lambdas that hold its registers by reference have to be inlined.
+#define EFQ_INLINE __attribute__((always_inline))
+
+// What brings the K and V tiles of one slot into LDS.  A tile's rows come in
+// pieces, one per load of a wave: where they lie is worked out for K and used
+// again for V, which follows a tile behind.
+template <int D, bool F8, int NW>
+struct ChunkFeed {
+  static constexpr int RB = F8 ? D : 2 * D;                 // bytes of a row
+  static constexpr int RI = 1024 / RB;                      // rows of a piece
+  static constexpr int PER = kBc / RI > NW ? kBc / RI / NW : 1;   // pieces of a wave
+  long at[2][PER];                                          // cache row of a piece: of K's tile, of the tile before
+  int rows[2][PER];                                         // rows of it that are keys
+  u32x4 kc[F8 ? PER : 1], vc[F8 ? PER : 1];                 // MXFP8: codes and scales on their way
+  unsigned ke[F8 ? PER : 1], ve[F8 ? PER : 1];
+  int off[2];                                               // bf16: the lane's place in a piece of K, of V
+
+  __device__ __forceinline__ void init(int wave, int lane) {
+    const int r = wave * PER * RI + lane * RI / 64, c = lane % (64 / RI);
+    off[0] = (lane * RI / 64) * RB + ((c ^ chunk_k_swz<D>(r)) << 4);
+    off[1] = (lane * RI / 64) * RB + ((c ^ chunk_v_swz<D>(r)) << 4);
+  }
+  // the swizzle of piece n against piece 0's: a bit of the row that n sets
+  template <int N>
+  static constexpr int turn(bool is_v) {
+    return is_v ? chunk_v_swz<D>(N * RI) << 4 : chunk_k_swz<D>(N * RI) << 4;
+  }
+  __device__ __forceinline__ static int first_row(int wave, int n) { return (F8 ? wave + n * NW : wave * PER + n) * RI; }
+  static constexpr bool kHalf = kBc / RI < NW;              // only some waves have a piece
+
+  // ids: lane 4 (tile % 16) + quarter has the page of that 16-key quarter
+  template <int N>
+  __device__ __forceinline__ void place(const PagedArgs& a, int h, int ids, int tile, int key0, int k1, int wave) {
+    const int r0 = first_row(wave, N);
+    const int id = __builtin_amdgcn_readlane(ids, (4 * (tile & 15) + r0 / 16) & 63);
+    const bool ok = (unsigned)id < (unsigned)a.b.pages;
+    at[1][N] = at[0][N];
+    rows[1][N] = rows[0][N];
+    const long p = (((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)(key0 + r0) & ((1u << a.b.shift) - 1));
+    at[0][N] = (long)((unsigned long long)(unsigned)uniform((int)(p >> 32)) << 32 | (unsigned)uniform((int)p));
+    rows[0][N] = uniform(ok ? min(max(k1 - key0 - r0, 0), RI) : 0);
+  }
+  // K (V = 0) or V (1) piece N of the tile that place (the one before) worked out
+  template <int N, int V>
+  __device__ __forceinline__ void ask(const PagedArgs& a, const uint8_t* to, int wave, int lane) {
+    const char* base = V ? a.vc : a.kc;
+    if constexpr (!F8) {
+      load_lds_1k(base + at[V][N] * RB, rows[V][N] * RB, lds_addr(to) + (wave * PER + N) * 1024, off[V] ^ turn<N>(V));
+    } else {
+      u32x4& c = V ? vc[N] : kc[N];
+      unsigned& e = V ? ve[N] : ke[N];
+      c = u32x4{0u, 0u, 0u, 0u};
+      e = 0u;
+      const int r = lane * RI / 64;
+      if (r < rows[V][N] && (!kHalf || wave * RI < kBc)) {
+        c = *(const u32x4*)(base + at[V][N] * RB + (unsigned)(16 * lane));
+        e = ((V ? a.vs : a.ks) + at[V][N] * (D / 32))[(unsigned)(r * (D / 32) + lane % (64 / RI) / 2)];
+      }
+    }
+  }
+  // MXFP8: what has come, as bf16, into the tile
+  template <int N, int V>
+  __device__ __forceinline__ void land(uint8_t* to, int wave, int lane) {
+    const int r = first_row(wave, N) + lane * RI / 64, c = lane % (64 / RI);
+    if (kHalf && wave * RI >= kBc) return;
+    const int swz = V ? chunk_v_swz<D>(r) : chunk_k_swz<D>(r);
+    const u32x4& x = V ? vc[N] : kc[N];
+    const float sc = e8m0_scale(V ? ve[N] : ke[N]);
+    const uint2 e = e4m3_bf16x4(x[0], sc), f = e4m3_bf16x4(x[1], sc);
+    const uint2 y = e4m3_bf16x4(x[2], sc), z = e4m3_bf16x4(x[3], sc);
+    *(u32x4*)(to + r * 2 * D + (((2 * c) ^ swz) << 4)) = u32x4{e.x, e.y, f.x, f.y};
+    *(u32x4*)(to + r * 2 * D + (((2 * c + 1) ^ swz) << 4)) = u32x4{y.x, y.y, z.x, z.y};
+  }
+};
+
+// The running reference of a row is its maximum, but for growth below 2^8: a
+// tile's probabilities may reach 2^8 before O and the sum are rescaled, which
+// costs no precision (their rounding is relative) and leaves out almost every
+// rescaling after the first tiles.
+constexpr float kGrowth = 8.0f;
 
 template <int D, bool F8, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
-  constexpr int BM = 32 * NW, KK = D / 16, DT = D / 32, kTile = ChunkLds<D>::kTile;
+  constexpr int BM = 32 * NW, KK = D / 16, DT = D / 32, kTile = ChunkLds<D, F8>::kTile, NB = ChunkLds<D, F8>::kRing;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
   const int h = blockIdx.x % a.Hkv, sp = blockIdx.y;
@@ -731,8 +835,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   const int ns = splits_of(a, s.keys);
   if (sp >= ns) return;
   const int last = min(s.keys, seen(a, s, s.rows - 1));
-  const int k0 = (int)min((long)sp * a.chunk, (long)s.keys);
-  const int k1 = max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk));
+  const int k0 = uniform((int)min((long)sp * a.chunk, (long)s.keys));
+  const int k1 = uniform(max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk)));
   const int ntiles = (k1 - k0 + kBc - 1) / kBc;
 
   const int r0 = 32 * wave, r = r0 + col;
@@ -744,7 +848,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
     for (int i = 0; i < KK; ++i) q[i] = *(const bf16x8*)(p + 32 * i + 16 * half);
   }
   const int vis = min(k1, seen(a, s, min(r, s.rows - 1)));
-  const int free_of_mask = min(k1, seen(a, s, min(r0, s.rows - 1)));   // keys below are seen by the wave's rows
+  const int free_of_mask = uniform(min(k1, seen(a, s, min(r0, s.rows - 1))));   // keys below are seen by the wave's rows
+  // tiles that some row of the wave sees
+  const int mine = uniform(r0 < s.rows ? (min(k1, seen(a, s, min(r0 + 31, s.rows - 1))) - k0 + kBc - 1) / kBc : 0);
   f32x16 o[DT];
 #pragma unroll
   for (int i = 0; i < DT; ++i)
@@ -752,159 +858,220 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
     for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
-  // lane 4 (tile % 16) + quarter: the page of that 16-key quarter of the tile
   const int32_t* table = a.b.table + (long)s.seq * a.b.width;
   auto pages_from = [&](int tile) {
     const long key = (long)k0 + (long)kBc * (tile + (lane >> 2)) + 16 * (lane & 3);
     return key < k1 ? table[key >> a.b.shift] : 0;
   };
   auto bad_of = [&](int ids) { return __builtin_amdgcn_ballot_w64((unsigned)ids >= (unsigned)a.b.pages); };
-  const unsigned in_page = (1u << a.b.shift) - 1;
 
-  constexpr int RI = 512 / D;                        // bf16 rows of a 1 KB load
-  constexpr int PER = kBc / RI / NW;                 // loads of a wave for K, and for V
-  constexpr int C8 = kBc * D / 16 / (64 * NW);       // MXFP8: 16-code pieces of a thread (0: half of them)
-  constexpr int N8 = C8 ? C8 : 1;
-  u32x4 kr[N8], vr[N8];                              // MXFP8: the next tile's codes
-  unsigned ksr[N8], vsr[N8];
-  auto fetch = [&](int tile, int ids, int buf) {
-    const int key0 = k0 + kBc * tile;
-    if constexpr (!F8) {
+  typedef ChunkFeed<D, F8, NW> Feed;
+  Feed feed;
+  feed.init(wave, lane);
+  auto k_tile = [&](int t) { return lds + (t % NB) * kTile; };
+  auto v_tile = [&](int t) { return lds + (NB + t % NB) * kTile; };
+
+  // offsets of the operands in a tile: K column chunk i, V head-dim tile i
+  const unsigned lds0 = lds_addr(lds);
+  unsigned ka[KK], va[DT];
 #pragma unroll
-      for (int n = 0; n < PER; ++n) {
-        const int ii = wave * PER + n, rr = ii * RI;             // first row of the load
-        const int id = __builtin_amdgcn_readlane(ids, 4 * (tile & 15) + rr / 16);
-        const bool ok = (unsigned)id < (unsigned)a.b.pages;
-        const long at = ((((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)(key0 + rr) & in_page)) * (2 * D);
-        const int rows = ok ? min(max(k1 - key0 - rr, 0), RI) : 0;
-        const int rw = rr + lane * RI / 64, c = lane % (64 / RI);
-        load_lds_1k(a.kc + at, rows * 2 * D, lds + buf * kTile + ii * 1024, (rw - rr) * 2 * D + ((c ^ chunk_k_swz<D>(rw)) << 4));
-        load_lds_1k(a.vc + at, rows * 2 * D, lds + (2 + buf) * kTile + ii * 1024, (rw - rr) * 2 * D + ((c ^ chunk_v_swz<D>(rw)) << 4));
-      }
-    } else {
+  for (int i = 0; i < KK; ++i) ka[i] = col * 2 * D + (((2 * i + half) ^ chunk_k_swz<D>(col)) << 4);
+  {
+    const int vr = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
-      for (int n = 0; n < N8; ++n) {
-        const int w0 = wave + n * NW;                            // 64 pieces: 1024 / D rows
-        constexpr int R8 = 1024 / D;
-        if (C8 == 0 && w0 * R8 >= kBc) break;
-        const int id = __builtin_amdgcn_readlane(ids, 4 * (tile & 15) + w0 * R8 / 16);
-        const bool ok = (unsigned)id < (unsigned)a.b.pages;
-        const int rw = w0 * R8 + lane * R8 / 64, c = lane % (64 / R8);
-        const long at = (((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)(key0 + w0 * R8) & in_page);
-        const bool live = ok && key0 + rw < k1;
-        const unsigned off = (rw - w0 * R8) * D + 16 * c, soff = (rw - w0 * R8) * (D / 32) + c / 2;
-        kr[n] = vr[n] = u32x4{0u, 0u, 0u, 0u};
-        ksr[n] = vsr[n] = 0u;
-        if (live) {
-          kr[n] = *(const u32x4*)(a.kc + at * D + off);
-          vr[n] = *(const u32x4*)(a.vc + at * D + off);
-          ksr[n] = (a.ks + at * (D / 32))[soff];
-          vsr[n] = (a.vs + at * (D / 32))[soff];
-        }
-      }
+    for (int i = 0; i < DT; ++i) {
+      const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+      va[i] = vr * 2 * D + ((c ^ chunk_v_swz<D>(vr)) << 4) + 8 * (lane & 1);
+    }
+  }
+
+  // Pages of tiles 16 grp .. 16 grp + 15 (ids) and of the next 16 (next), with
+  // a bit for each quarter whose page is none; j's group is grp.
+  // They are asked for 8 tiles before they are taken over, in a register of
+  // their own, so that only the taking over waits for them.
+  int ids = 0, next = 0, asked = 0, grp = 0;
+  unsigned long long bad = 0, next_bad = 0;
+  auto turn_page = [&](int j) EFQ_INLINE {
+    if ((j & 15) == 8) {
+      next = asked;
+      next_bad = bad_of(next);
+    }
+    if ((j & 15) == 0 && j > 0) {
+      ids = next;
+      bad = next_bad;
+      asked = pages_from(j + 16);
+      ++grp;
     }
   };
-  auto land = [&](int buf) {
+  // Piece I of what a step brings: K tile t (the first PER), V tile t - 1.
+  // Past the last tile the loads go on, of no bytes, so that a wait counts the
+  // same loads in every step.
+  auto fetch_one = [&](auto piece, int t) EFQ_INLINE {
+    constexpr int I = decltype(piece)::value;
+    if constexpr (I < Feed::PER) {
+      feed.template place<I>(a, h, t >> 4 == grp ? ids : next, t, k0 + kBc * t, k1, wave);
+      feed.template ask<I, 0>(a, k_tile(t), wave, lane);
+    } else {
+      feed.template ask<I - Feed::PER, 1>(a, v_tile(t - 1), wave, lane);
+    }
+  };
+  auto fetch_k = [&](int t) EFQ_INLINE { static_for<Feed::PER>([&](auto i) EFQ_INLINE { fetch_one(i, t); }); };
+  auto fetch = [&](int t) EFQ_INLINE { static_for<2 * Feed::PER>([&](auto i) EFQ_INLINE { fetch_one(i, t); }); };
+  auto land_k = [&](int t) EFQ_INLINE {
+    if constexpr (F8)
+      static_for<Feed::PER>([&](auto i) EFQ_INLINE { feed.template land<decltype(i)::value, 0>(k_tile(t), wave, lane); });
+  };
+  auto land = [&](int t) EFQ_INLINE {                       // K tile t, V tile t - 1
     if constexpr (F8) {
-#pragma unroll
-      for (int n = 0; n < N8; ++n) {
-        constexpr int R8 = 1024 / D;
-        const int w0 = wave + n * NW;
-        if (C8 == 0 && w0 * R8 >= kBc) break;
-        const int rw = w0 * R8 + lane * R8 / 64, c = lane % (64 / R8);
-        auto put = [&](uint8_t* tile, u32x4 x, float sc, int swz) {
-          const uint2 e = e4m3_bf16x4(x[0], sc), f = e4m3_bf16x4(x[1], sc);
-          const uint2 y = e4m3_bf16x4(x[2], sc), z = e4m3_bf16x4(x[3], sc);
-          *(u32x4*)(tile + rw * 2 * D + (((2 * c) ^ swz) << 4)) = u32x4{e.x, e.y, f.x, f.y};
-          *(u32x4*)(tile + rw * 2 * D + (((2 * c + 1) ^ swz) << 4)) = u32x4{y.x, y.y, z.x, z.y};
-        };
-        put(lds + buf * kTile, kr[n], e8m0_scale(ksr[n]), chunk_k_swz<D>(rw));
-        put(lds + (2 + buf) * kTile, vr[n], e8m0_scale(vsr[n]), chunk_v_swz<D>(rw));
-      }
-    } else {
-      wait_vmem();
+      land_k(t);
+      static_for<Feed::PER>([&](auto i) EFQ_INLINE { feed.template land<decltype(i)::value, 1>(v_tile(t - 1), wave, lane); });
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-    __syncthreads();
   };
 
-  if (ntiles > 0) {
-    int ids = pages_from(0), next = pages_from(16);
-    unsigned long long bad = bad_of(ids), next_bad = bad;
-    fetch(0, ids, 0);
-    land(0);
-    for (int j = 0; j < ntiles; ++j) {
-      const int buf = j & 1, key0 = k0 + kBc * j;
-      const unsigned now_bad = (unsigned)(bad >> (4 * (j & 15))) & 15u;
-      if (j + 1 < ntiles) {
-        if (((j + 1) & 15) == 0) {
-          ids = next;
-          bad = bad_of(ids);
-          next = pages_from(j + 17);
+  f32x16 sc[2];
+  bf16x8 p[4];
+  auto scores = [&](int t) EFQ_INLINE {
+    const unsigned kt = lds0 + t % NB * kTile;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sc[w][i] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < KK; ++i) {
+        const bf16x8 kop = *(__attribute__((address_space(3))) const bf16x8*)(lds_at(kt + ka[i]) + w * 64 * D);
+        sc[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, q[i], sc[w], 0, 0, 0);
+      }
+    }
+  };
+  // M(j) is NV products of V tile j with its probabilities, then NK of K tile
+  // j + 1 with Q.  Their operands are read kAhead products before they are used
+  // (an LDS read takes as long as about four products), the first ones at the
+  // end of the vector phase before.
+  constexpr int NV = 4 * DT, NK = 2 * KK, kAhead = 4;
+  bf16x8 op[NV + NK];
+  auto read_op = [&](auto n, unsigned kt, unsigned vt) EFQ_INLINE {
+    constexpr int N = decltype(n)::value;
+    if constexpr (N < NV) {
+      const lds_cptr at = lds_at(vt + va[N % DT]) + (N / DT) * 32 * D;
+      const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+      const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * D));
+      op[N] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    } else if constexpr (N < NV + NK) {
+      constexpr int I = N - NV;
+      op[N] = *(__attribute__((address_space(3))) const bf16x8*)(lds_at(kt + ka[I / 2]) + (I % 2) * 64 * D);
+    }
+  };
+  auto tiles_at = [&](int j, unsigned& kt, unsigned& vt) EFQ_INLINE {
+    kt = lds0 + (j + 1) % NB * kTile;
+    vt = lds0 + (NB + j % NB) * kTile;
+  };
+  auto first_ops = [&](int j) EFQ_INLINE {
+    unsigned kt, vt;
+    tiles_at(j, kt, vt);
+    static_for<kAhead>([&](auto n) EFQ_INLINE { read_op(n, kt, vt); });
+  };
+  // The step's loads are asked for between products, in whose shadow the scalar
+  // work of finding their addresses costs nothing.
+  auto phase_m = [&](int j) EFQ_INLINE {
+    if (j >= mine) return fetch(j + NB);
+    unsigned kt, vt;
+    tiles_at(j, kt, vt);
+    static_for<NV + NK>([&](auto n) EFQ_INLINE {
+      constexpr int N = decltype(n)::value;
+      if constexpr (N < NV) {
+        o[N % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[N], p[N / DT], o[N % DT], 0, 0, 0);
+      } else {
+        constexpr int I = N - NV, W = I % 2;
+        if constexpr (I < 2) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sc[W][i] = 0.0f;
         }
-        fetch(j + 1, ids, buf ^ 1);
+        sc[W] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[N], q[I / 2], sc[W], 0, 0, 0);
       }
-      const uint8_t* kt = lds + buf * kTile;
-      const uint8_t* vt = lds + (2 + buf) * kTile;
-      f32x16 sc[2];
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sc[w][i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < KK; ++i) {
-          const int kr_ = 32 * w + col;
-          const bf16x8 kop = *(const bf16x8*)(kt + kr_ * 2 * D + (((2 * i + half) ^ chunk_k_swz<D>(kr_)) << 4));
-          sc[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, q[i], sc[w], 0, 0, 0);
-        }
-      }
-      if (now_bad || key0 + kBc > free_of_mask) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int kw = 32 * w + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (key0 + kw >= vis || (now_bad >> (2 * w + (i >> 3)) & 1)) sc[w][i] = -INFINITY;
-          }
-      }
-      const float mx = max_of_halves(__builtin_fmaxf(max16(sc[0]), max16(sc[1]))) * a.sl2;
-      if (__builtin_amdgcn_ballot_w64(mx > m)) {
-        const float mn = __builtin_fmaxf(m, mx);
-        const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
-        m = mn;
-        l *= alpha;
-#pragma unroll
-        for (int i = 0; i < DT; ++i) o[i] *= alpha;
-      }
-      const float ref = m == -INFINITY ? 0.0f : m;
+      read_op(std::integral_constant<int, N + kAhead>{}, kt, vt);
+      constexpr int kEvery = (NV + NK) / (2 * Feed::PER);
+      if constexpr (N % kEvery == kEvery / 2) fetch_one(std::integral_constant<int, N / kEvery>{}, j + NB);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  auto phase_v = [&](int j) EFQ_INLINE {                    // probabilities of tile j
+    if (j >= mine) return;
+    const int key0 = k0 + kBc * j;
+    const unsigned none = (unsigned)((j >> 4 == grp ? bad : next_bad) >> (4 * (j & 15))) & 15u;
+    if (none || key0 + kBc > free_of_mask) {
 #pragma unroll
       for (int w = 0; w < 2; ++w)
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-          u32x4 pw;
-          float sum = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[w][8 * ks + 2 * i], a.sl2, -ref));
-            const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[w][8 * ks + 2 * i + 1], a.sl2, -ref));
-            sum += e0 + e1;
-            pw[i] = pack_bf16(e0, e1);
-          }
-          l += sum;
-          const bf16x8 p = __builtin_bit_cast(bf16x8, pw);
-          const int vr0 = 32 * w + 16 * ks + 4 * half + ((lane & 15) >> 2);
-#pragma unroll
-          for (int i = 0; i < DT; ++i) {
-            const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1), b = 8 * (lane & 1);
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s16x4*)(vt + vr0 * 2 * D + ((c ^ chunk_v_swz<D>(vr0)) << 4) + b));
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_s16x4*)(vt + (vr0 + 8) * 2 * D + ((c ^ chunk_v_swz<D>(vr0 + 8)) << 4) + b));
-            const bf16x8 vop = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-            o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vop, p, o[i], 0, 0, 0);
-          }
+        for (int i = 0; i < 16; ++i) {
+          const int kw = 32 * w + 8 * (i >> 2) + 4 * half + (i & 3);
+          if (key0 + kw >= vis || (none >> (2 * w + (i >> 3)) & 1)) sc[w][i] = -INFINITY;
         }
-      land(buf ^ 1);
     }
+    const float mx = max_of_halves(__builtin_fmaxf(max16(sc[0]), max16(sc[1]))) * a.sl2;
+    if (__builtin_amdgcn_ballot_w64(mx > m + kGrowth)) {
+      const float mn = __builtin_fmaxf(m, mx);
+      const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= alpha;
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      u32x4 pw;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x16& x = sc[ks / 2];
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[8 * (ks & 1) + 2 * i], a.sl2, -ref));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[8 * (ks & 1) + 2 * i + 1], a.sl2, -ref));
+        sum += e0 + e1;
+        pw[i] = pack_bf16(e0, e1);
+      }
+      l += sum;
+      p[ks] = __builtin_bit_cast(bf16x8, pw);
+    }
+    first_ops(j);
+  };
+
+  // The second group runs a phase behind the first.  bf16, step j: K tile
+  // j + NB and V tile j + NB - 1 are asked for in M(j), into the places of tiles
+  // j and j - 1, which both groups have read by then; before the barrier behind
+  // M(j) a wave waits for its part of K tile j + 3 and V tile j + 2: the first
+  // group begins to read K tile j + 2 and V tile j + 1 in the phase after.  MXFP8 (NB = 3): K tile j + 3 and V tile j + 2 come into
+  // registers in M(j) and are written in V(j + 1).
+  constexpr int kLoads = 2 * Feed::PER;                     // of a wave in a step
+  if (ntiles > 0) {
+    ids = pages_from(0);
+    asked = pages_from(16);
+    bad = bad_of(ids);
+    fetch_k(0);
+    land_k(0);
+#pragma unroll
+    for (int t = 1; t < NB; ++t) {
+      fetch(t);
+      land(t);
+    }
+    if constexpr (!F8) wait_vmem_le((NB - 3) * kLoads);
+    wg_barrier();
+    if (mine > 0) scores(0);
+    phase_v(0);
+    wg_barrier();                                           // K tile 0 is read before its place is filled again
+    const bool second = wave >= NW / 2;
+    if (second) wg_barrier();
+    for (int j = 0; j < ntiles; ++j) {
+      turn_page(j);
+      phase_m(j);
+      if constexpr (!F8) wait_vmem_le((NB - 3) * kLoads);
+      wg_barrier();
+      if (j + 1 < ntiles) phase_v(j + 1);
+      land(j + NB);
+      wg_barrier();
+    }
+    if (!second) wg_barrier();
+    if constexpr (!F8) wait_vmem();                         // nothing is on its way to LDS when it is given up
   }
   l = sum_of_halves(l);
   if (r >= s.rows) return;
@@ -1148,7 +1315,7 @@ hipError_t launch_step(const PagedArgs& a, dim3 grid, hipStream_t st) {
 }
 template <int D, bool F8, int NW>
 hipError_t launch_chunk(const PagedArgs& a, dim3 grid, hipStream_t st) {
-  constexpr int lds = ChunkLds<D>::kTotal;
+  constexpr int lds = ChunkLds<D, F8>::kTotal;
   const hipError_t e = raise_lds_of<(D * 2 + F8) * 8>((const void*)paged_chunk_kernel<D, F8, NW>, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((paged_chunk_kernel<D, F8, NW>), grid, dim3(64 * NW), lds, st, a);
