@@ -326,11 +326,13 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // -------------------------------------------------------- paged attention
 // Rows: the new tokens of one sequence times the G query heads that share a
 // key/value head, row r = token r / G, head h G + r % G.  A workgroup takes
-// BM of them ("slot"): slot n of the call belongs to the last sequence i with
-// floor(q_start[i] G / BM) + i <= n, so that a sequence has at least
-// ceil(new G / BM) slots whatever the lengths, and the grid, which the host
-// knows without reading them, is floor(tokens G / BM) + seqs; slots without
-// rows leave at once.
+// BM of them at a time.  In the step kernel, where the host knows of no sequence
+// with more than BM rows, slot n of the grid is sequence n, whose workgroup goes
+// on to further BM rows if there are any.  Otherwise slot n belongs to the last sequence i with
+// floor((q_start[i] - q_start[0]) G / BM) + i <= n, so that a sequence has at
+// least ceil(new G / BM) slots whatever the lengths, and the grid, which the
+// host knows without reading them, is ceil(tokens G / BM) + seqs - 1; slots
+// without rows leave at once.
 //
 // Both kernels compute scores transposed, S^T = K Q^T, so a lane owns one row
 // (column of the product), and O^T += V^T P^T with P^T taken from the score
@@ -352,6 +354,7 @@ struct PagedArgs {
   float sl2;                               // scale log2 e
   int Hq, Hkv, G, causal, out_f32;
   int nsplit, chunk;                       // most splits of a row, keys of one
+  int direct;                              // a slot is a sequence
   long rows;                               // tokens * Hq
   float* part_o;                           // [nsplit][rows][D]
   float2* part_ml;                         // [nsplit][rows]: maximum (log2 units), sum
@@ -365,14 +368,29 @@ struct Slot {
 // ask for by then.
 template <int BM>
 __device__ __forceinline__ bool find_slot(const PagedArgs& a, int n, Slot& s) {
-  auto at = [&](int i, int start) { return (long)start * a.G / BM + i; };
   int end;
-  s.seq = last_at_most(a.b, n, at, s.q0, end);
-  if (s.seq < 0) return false;
+  if (a.direct) {
+    s.seq = n;
+    s.q0 = a.b.start(n);
+    end = a.b.start(n + 1);
+    s.row0 = 0;
+  } else {
+    const int origin = a.b.start(0);
+    auto at = [&](int i, int start) { return (long)max(start - origin, 0) * a.G / BM + i; };
+    s.seq = last_at_most(a.b, n, at, s.q0, end);
+    if (s.seq < 0) return false;
+    s.row0 = (int)(n - at(s.seq, s.q0)) * BM;
+  }
   s.new_ = max(end - s.q0, 0);
-  s.row0 = (int)(n - at(s.seq, s.q0)) * BM;
   s.rows = min(BM, s.new_ * a.G - s.row0);
   return s.rows > 0;
+}
+// On to the sequence's next rows.
+template <int BM>
+__device__ __forceinline__ bool next_rows(const PagedArgs& a, Slot& s) {
+  s.row0 += BM;
+  s.rows = min(BM, s.new_ * a.G - s.row0);
+  return a.direct && s.rows > 0;
 }
 
 // Keys that row r of the slot sees.
@@ -498,16 +516,15 @@ __device__ __forceinline__ int step_q_col(int g, int s) {
   return F8 ? 64 * (s / 2) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
 }
 
+// One slot's rows, split sp of their keys.
 template <int D, bool F8, int RT>
-__global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArgs a) {
-  extern __shared__ __align__(16) uint8_t lds[];
+__device__ __forceinline__ void step_rows(const PagedArgs& a, Slot& s, int h, int sp, uint8_t* lds) {
   typedef StepLds<D, RT> L;
   constexpr int KS = D / 32, SLABS = D / 16, KEYS = 16 * kStepHalves, ROUND = kStepWaves * KEYS, AHEAD = 64 / kStepHalves;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  int lane = threadIdx.x & 63;
+  asm volatile("" : "+v"(lane));           // nothing of it is kept from one round of rows to the next
+  const int wave = uniform(threadIdx.x >> 6);
   const int g = lane >> 4, col = lane & 15;
-  const int h = blockIdx.x % a.Hkv, sp = blockIdx.y;
-  Slot s;
-  if (!find_slot<16 * RT>(a, (int)(blockIdx.x / a.Hkv), s)) return;
 
   // The wave's tiles begin at k0 + KEYS wave + ROUND it; lane kStepHalves (it % AHEAD) +
   // half holds the page of that tile's half, for AHEAD tiles at a time.  The
@@ -695,6 +712,18 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
   }
 }
 
+template <int D, bool F8, int RT>
+__global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int h = blockIdx.x % a.Hkv;
+  Slot s;
+  if (!find_slot<16 * RT>(a, (int)(blockIdx.x / a.Hkv), s)) return;
+  do {
+    step_rows<D, F8, RT>(a, s, h, (int)blockIdx.y, lds);
+    __syncthreads();
+  } while (next_rows<16 * RT>(a, s));
+}
+
 // ---- many tokens
 // Waves of 32 rows share 64-key tiles of K and V in LDS, two of each.  A SIMD
 // overlaps its matrix core and its vector unit when one of its two waves does
@@ -711,10 +740,10 @@ __device__ __forceinline__ void static_for(F&& f) {
   }
 }
 
-template <int D, bool F8>
+template <int D, bool F8, int NW>
 struct ChunkLds {
   static constexpr int kTile = kBc * D * 2;     // bytes of 64 rows of K or V
-  static constexpr int kRing = F8 ? 3 : 4;      // tiles of each
+  static constexpr int kRing = F8 || NW == 4 ? 3 : 4;   // tiles of each
   static constexpr int kTotal = 2 * kRing * kTile;
 };
 
@@ -821,16 +850,12 @@ struct ChunkFeed {
 // rescaling after the first tiles.
 constexpr float kGrowth = 8.0f;
 
+// One slot's rows, split sp of their keys.
 template <int D, bool F8, int NW>
-__global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
-  extern __shared__ __align__(16) uint8_t lds[];
-  constexpr int BM = 32 * NW, KK = D / 16, DT = D / 32, kTile = ChunkLds<D, F8>::kTile, NB = ChunkLds<D, F8>::kRing;
+__device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, int sp, uint8_t* lds) {
+  constexpr int KK = D / 16, DT = D / 32, kTile = ChunkLds<D, F8, NW>::kTile, NB = ChunkLds<D, F8, NW>::kRing;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
-  const int h = blockIdx.x % a.Hkv, sp = blockIdx.y;
-  Slot s;
-  // the last slots see the most keys: first
-  if (!find_slot<BM>(a, (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), s)) return;
   s.keys = a.b.keys(s.seq);
   const int ns = splits_of(a, s.keys);
   if (sp >= ns) return;
@@ -975,6 +1000,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   // work of finding their addresses costs nothing.
   auto phase_m = [&](int j) EFQ_INLINE {
     if (j >= mine) return fetch(j + NB);
+    __builtin_amdgcn_s_setprio(1);
     unsigned kt, vt;
     tiles_at(j, kt, vt);
     static_for<NV + NK>([&](auto n) EFQ_INLINE {
@@ -997,6 +1023,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   };
   auto phase_v = [&](int j) EFQ_INLINE {                    // probabilities of tile j
     if (j >= mine) return;
+    __builtin_amdgcn_s_setprio(0);
     const int key0 = k0 + kBc * j;
     const unsigned none = (unsigned)((j >> 4 == grp ? bad : next_bad) >> (4 * (j & 15))) & 15u;
     if (none || key0 + kBc > free_of_mask) {
@@ -1043,6 +1070,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
   // group begins to read K tile j + 2 and V tile j + 1 in the phase after.  MXFP8 (NB = 3): K tile j + 3 and V tile j + 2 come into
   // registers in M(j) and are written in V(j + 1).
   constexpr int kLoads = 2 * Feed::PER;                     // of a wave in a step
+  constexpr bool PAIR = NW == 8;
+  constexpr int kKept = (PAIR ? NB - 3 : NB - 2) * kLoads;  // of them on their way at a wait
   if (ntiles > 0) {
     ids = pages_from(0);
     asked = pages_from(16);
@@ -1054,23 +1083,23 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
       fetch(t);
       land(t);
     }
-    if constexpr (!F8) wait_vmem_le((NB - 3) * kLoads);
+    if constexpr (!F8) wait_vmem_le(kKept);
     wg_barrier();
     if (mine > 0) scores(0);
     phase_v(0);
     wg_barrier();                                           // K tile 0 is read before its place is filled again
-    const bool second = wave >= NW / 2;
+    const bool second = PAIR && wave >= NW / 2;
     if (second) wg_barrier();
     for (int j = 0; j < ntiles; ++j) {
       turn_page(j);
       phase_m(j);
-      if constexpr (!F8) wait_vmem_le((NB - 3) * kLoads);
+      if constexpr (!F8) wait_vmem_le(kKept);
       wg_barrier();
       if (j + 1 < ntiles) phase_v(j + 1);
       land(j + NB);
-      wg_barrier();
+      if constexpr (PAIR) wg_barrier();
     }
-    if (!second) wg_barrier();
+    if (PAIR && !second) wg_barrier();
     if constexpr (!F8) wait_vmem();                         // nothing is on its way to LDS when it is given up
   }
   l = sum_of_halves(l);
@@ -1096,6 +1125,16 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_chunk_kernel(PagedArgs a) {
         *(f32x4*)(p + 32 * i + 8 * j + 4 * half) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
     if (half == 0) a.part_ml[(long)sp * a.rows + at] = make_float2(m, l);
   }
+}
+
+template <int D, bool F8, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 && !F8 ? 3 : 2) void paged_chunk_kernel(PagedArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int h = blockIdx.x % a.Hkv;
+  Slot s;
+  // the last slots see the most keys: first
+  if (!find_slot<32 * NW>(a, (int)(gridDim.x / a.Hkv) - 1 - (int)(blockIdx.x / a.Hkv), s)) return;
+  chunk_rows<D, F8, NW>(a, s, h, (int)blockIdx.y, lds);
 }
 
 // W waves (1 or 4) per row that ran split: the parts, weighted to the common
@@ -1246,6 +1285,7 @@ void token_grid(int tokens, int threads_per_token, int& tt, int& parts) {
 struct PagedPlan {
   int rt;              // 1, 2: step kernel with 16 rt rows; 0: chunk kernel
   int bm, nsplit, chunk;
+  bool direct;         // a slot is a sequence
   long slots;
   size_t bytes;
 };
@@ -1254,29 +1294,41 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
   const int G = heads_q / c->heads_kv;
   const long most_q = b->max_q ? b->max_q : std::max<long>(1, (long)b->tokens - b->seqs + 1);
   const long rows = most_q * G;
-  p.rt = rows <= 16 ? 1 : rows <= 64 ? 2 : 0;
-  p.bm = p.rt ? 16 * p.rt : 256;
-  p.slots = (long)b->tokens * G / p.bm + b->seqs;
+  // The chunk kernel's waves share what they read, the step kernel's rows all
+  // pass through every wave.  32 rows: 16 sequences x 8 tokens over 4000 keys
+  // (32/8 heads, D 128, bf16) step 42 us, chunk 51; 64 rows: x 16 tokens 58 and
+  // 53, MXFP8 41 and 55; D 64, 4 sequences x 16 tokens 13.9 and 19.0.
+  const bool low = c->format == EFQ_CACHE_MXFP8, narrow = c->head_dim == 64;
+  p.rt = rows <= 16 ? 1 : rows <= (low || narrow ? 64 : 32) ? 2 : 0;
+  p.bm = p.rt ? 16 * p.rt : narrow ? 128 : 256;
+  p.direct = p.rt && rows <= p.bm;
+  p.slots = p.direct ? b->seqs : ((long)b->tokens * G + p.bm - 1) / p.bm + b->seqs - 1;
   const long keys = std::min({(long)b->table_width * c->page_size, (long)kMostKeys, b->max_k ? (long)b->max_k : (long)kMostKeys});
-  const long items = std::max<long>(1, p.slots * c->heads_kv);
-  // Splits of the longest sequence.  Step kernel: as many as put two
-  // workgroups on every CU; sequences of different lengths (more than one)
-  // also want pieces small enough to end together, down to 448 KB of keys and
-  // values, which stream in about ten times what it takes to start a
-  // workgroup.  17 sequences of 5000 to 20000 keys (32/8 heads, D 128, bf16) in
-  // pieces of 6700 / 2900 / 1540 / 830 keys: 164 / 171 / 145 / 138 us; one of
-  // 131000 keys in 64 / 256 pieces 87 / 98 us.  No piece is below 512 keys: its
-  // join would cost more than it saves (one sequence of 500 keys in two 15.0
-  // us, in one 10.9).
-  long n;
+  long n = 1;
   if (p.rt) {
-    const long key_bytes = 2 * (c->format == EFQ_CACHE_BF16 ? 2 * c->head_dim : c->head_dim + c->head_dim / 32);
+    // Splits of the longest sequence: as many as put two workgroups on every
+    // CU; sequences of different lengths (more than one) also want pieces small
+    // enough to end together, down to 448 KB of keys and values, which stream in
+    // about ten times what it takes to start a workgroup.  17 sequences of 5000
+    // to 20000 keys (32/8 heads, D 128, bf16) in pieces of 6700 / 2900 / 1540 /
+    // 830 keys: 164 / 171 / 145 / 138 us; one of 131000 keys in 64 / 256 pieces
+    // 87 / 98 us.  Below 1024 keys the join costs more than it saves (one
+    // sequence of 500 keys in two 15.0 us, in one 10.9; of 2000 in 4 / 8 pieces
+    // 14.6 / 12.9).
+    const long items = std::max<long>(1, p.slots * c->heads_kv);
+    const long key_bytes = 2 * (low ? c->head_dim + c->head_dim / 32 : 2 * c->head_dim);
     n = (2 * kCUs + items - 1) / items;
     if (b->seqs > 1) n = std::max(n, keys * key_bytes / (448 << 10));
+    n = keys < 1024 ? 1 : std::max<long>(1, std::min(n, keys / 256));
   } else {
-    n = (kCUs + items - 1) / items;
+    // As many pieces (of at least 256 keys) as leave the chip one round of
+    // workgroups, by the average of the sequences' rows; rounded up where lengths
+    // differ, since short sequences fill fewer.  64 tokens over 20000 keys (32/8 heads, D 128, bf16: 8
+    // workgroups unsplit) in 8 / 16 / 32 pieces 79 / 54 / 47 us, 700 tokens over
+    // 20000 (88) in 1 / 2 / 3 / 4 pieces 479 / 283 / 370 / 306.
+    const long items = b->seqs * (((long)b->tokens * G / b->seqs + p.bm - 1) / p.bm) * c->heads_kv;
+    n = std::max<long>(1, std::min((kCUs + (b->seqs > 1 ? items / 2 : 0)) / std::max<long>(1, items), keys / 256));
   }
-  n = std::max<long>(1, std::min(n, keys / 512));
   p.chunk = (int)(((keys + n - 1) / n + 127) / 128 * 128);
   p.nsplit = (int)std::max<long>(1, (keys + p.chunk - 1) / p.chunk);
   p.bytes = p.nsplit == 1 ? 0 : round256((size_t)p.nsplit * b->tokens * heads_q * 8) +
@@ -1315,7 +1367,7 @@ hipError_t launch_step(const PagedArgs& a, dim3 grid, hipStream_t st) {
 }
 template <int D, bool F8, int NW>
 hipError_t launch_chunk(const PagedArgs& a, dim3 grid, hipStream_t st) {
-  constexpr int lds = ChunkLds<D, F8>::kTotal;
+  constexpr int lds = ChunkLds<D, F8, NW>::kTotal;
   const hipError_t e = raise_lds_of<(D * 2 + F8) * 8>((const void*)paged_chunk_kernel<D, F8, NW>, lds);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((paged_chunk_kernel<D, F8, NW>), grid, dim3(64 * NW), lds, st, a);
@@ -1326,7 +1378,7 @@ hipError_t launch_paged(const PagedArgs& a, const PagedPlan& p, hipStream_t st) 
   const dim3 grid((unsigned)(p.slots * a.Hkv), (unsigned)a.nsplit);
   const hipError_t e = p.rt == 1 ? launch_step<D, F8, 1>(a, grid, st)
                      : p.rt == 2 ? launch_step<D, F8, 2>(a, grid, st)
-                                 : launch_chunk<D, F8, 8>(a, grid, st);
+                                 : launch_chunk<D, F8, D == 64 ? 4 : 8>(a, grid, st);
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int W = a.nsplit > 4 ? 4 : 1;
   hipLaunchKernelGGL(paged_merge_kernel<D>, dim3((unsigned)(W == 4 ? a.rows : (a.rows + 3) / 4)), dim3(256), 0, st, a, W);
@@ -1461,7 +1513,7 @@ int efq_attn_paged(const efq_rows* q, int heads_q, const efq_cache* cache, const
   a.causal = causal != 0, a.out_f32 = out_dtype == EFQ_F32;
   a.rows = (long)batch->tokens * heads_q;
   if (ws_bytes < p.bytes) p.nsplit = 1, p.chunk = 0x7fffff00;
-  a.nsplit = p.nsplit, a.chunk = p.chunk;
+  a.nsplit = p.nsplit, a.chunk = p.chunk, a.direct = p.direct;
   a.part_ml = (float2*)ws;
   a.part_o = (float*)((uint8_t*)ws + round256((size_t)p.nsplit * a.rows * 8));
   hipStream_t st = (hipStream_t)stream;
