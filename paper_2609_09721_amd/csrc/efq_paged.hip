@@ -94,48 +94,62 @@ struct RopeArgs {
   const char* x;
   char* y;
   long x_token, x_head, y_token, y_head;   // bytes
-  int tokens, heads, chunks;               // chunks of 16 values of a head
+  int tokens, heads, chunks;               // chunks: items of a head
   int tt;                                  // tokens of a workgroup
+  int dt, dh, dc;                          // one step of the workgroups of a token, in tokens, heads, chunks
   int inverse;
   RotArgs rot;
 };
 
-// Sixteen values of a head, as fp32: 8 at lo and 8 at hi (bytes).
+// What is read once asks the caches not to keep it: one token over 131000 keys
+// (32/8 heads, D 128, bf16) 99.9 -> 87.5 us (5.37 -> 6.13 TB/s), 300 tokens over
+// 1000 keys each 141 -> 131 us.
+__device__ __forceinline__ u32x4 stream16(const char* p) { return __builtin_nontemporal_load((const u32x4*)p); }
+
+// The values of 16-byte pieces.
 template <bool F32>
-__device__ __forceinline__ void load16(const char* lo, const char* hi, float* v) {
-  if constexpr (F32) {
-    const f32x4 a = *(const f32x4*)lo, b = *(const f32x4*)(lo + 16);
-    const f32x4 c = *(const f32x4*)hi, d = *(const f32x4*)(hi + 16);
+struct Piece {
+  static constexpr int E = F32 ? 4 : 8;
+  u32x4 w;
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (F32) return __uint_as_float(w[i]);
+    else return i & 1 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]);
+  }
+  __device__ __forceinline__ void set2(int i, float u, float v) {    // values i and i + 1, i even
+    if constexpr (F32) w[i] = __float_as_uint(u), w[i + 1] = __float_as_uint(v);
+    else w[i / 2] = pack_bf16(u, v);
+  }
+};
+// A piece of neighbouring pairs.
+template <bool F32>
+__device__ __forceinline__ void turn_beside(Piece<F32>& p, const float2* cs) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i], v[8 + i] = c[i], v[12 + i] = d[i];
-  } else {
-    const u32x4 a = *(const u32x4*)lo, b = *(const u32x4*)hi;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      v[2 * i] = bf16_lo(a[i]), v[2 * i + 1] = bf16_hi(a[i]), v[8 + 2 * i] = bf16_lo(b[i]), v[9 + 2 * i] = bf16_hi(b[i]);
+  for (int j = 0; j < Piece<F32>::E / 2; ++j) {
+    const float2 c = cs[j];
+    const float u = p.get(2 * j), v = p.get(2 * j + 1);
+    p.set2(2 * j, __builtin_fmaf(u, c.x, -(v * c.y)), __builtin_fmaf(v, c.x, u * c.y));
   }
 }
+// Two pieces, the first and second values of the same pairs.
 template <bool F32>
-__device__ __forceinline__ void store16(char* lo, char* hi, const float* v) {
-  if constexpr (F32) {
-    *(f32x4*)lo = f32x4{v[0], v[1], v[2], v[3]};
-    *(f32x4*)(lo + 16) = f32x4{v[4], v[5], v[6], v[7]};
-    *(f32x4*)hi = f32x4{v[8], v[9], v[10], v[11]};
-    *(f32x4*)(hi + 16) = f32x4{v[12], v[13], v[14], v[15]};
-  } else {
-    u32x4 a, b;
+__device__ __forceinline__ void turn_halves(Piece<F32>& lo, Piece<F32>& hi, const float2* cs) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = pack_bf16(v[2 * i], v[2 * i + 1]), b[i] = pack_bf16(v[8 + 2 * i], v[9 + 2 * i]);
-    *(u32x4*)lo = a;
-    *(u32x4*)hi = b;
+  for (int j = 0; j < Piece<F32>::E; j += 2) {
+    const float2 c = cs[j], d = cs[j + 1];
+    const float u = lo.get(j), v = hi.get(j), x = lo.get(j + 1), y = hi.get(j + 1);
+    lo.set2(j, __builtin_fmaf(u, c.x, -(v * c.y)), __builtin_fmaf(x, d.x, -(y * d.y)));
+    hi.set2(j, __builtin_fmaf(v, c.x, u * c.y), __builtin_fmaf(y, d.x, x * d.y));
   }
 }
 
 constexpr int kRopeTokens = 8;     // most tokens of a workgroup
 constexpr int kRopePairs = 256;    // most pairs of a head
 
-// A thread turns 8 pairs of one head: pairs 8 c .. 8 c + 7 of chunk c, each of
-// its values read once.  Chunks behind the pairs pass through.
+// An item is a 16-byte piece of a head (neighbouring pairs) or the two pieces of
+// the same pairs (halves), so that the lanes of a load lie side by side; pieces
+// behind the pairs pass through.  Every value is read once, past the caches.  A
+// thread has several items on their way at once, found by stepping (token, head,
+// chunk) on, since a division an item would cost as much as the turn.
 template <bool F32, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 rot[];          // [tt][pairs]
@@ -145,29 +159,43 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   for (int i = threadIdx.x; i < nt * pairs; i += 256)
     rot[i] = rot_of(a.rot, t0 + i / pairs, i % pairs, a.inverse);
   __syncthreads();
-  constexpr int ES = F32 ? 4 : 2;
-  const int per = a.heads * a.chunks, turned = pairs / 8;
-  const int part = gridDim.y;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * per; i += 256 * part) {
-    const int t = i / per, r = i % per, h = r / a.chunks, c = r % a.chunks;
-    const char* x = a.x + (t0 + t) * a.x_token + h * a.x_head;
-    char* y = a.y + (t0 + t) * a.y_token + h * a.y_head;
-    const bool turn = c < turned;
-    const bool half = !INTERLEAVED && turn;
-    const int lo = (half ? 8 * c : 16 * c) * ES, hi = (half ? pairs + 8 * c : 16 * c + 8) * ES;
-    float v[16];
-    load16<F32>(x + lo, x + hi, v);
-    if (turn) {
-      const float2* cs = rot + t * pairs + 8 * c;
+  constexpr int E = Piece<F32>::E, U = INTERLEAVED ? 4 : 2;
+  const int per = a.heads * a.chunks, first = blockIdx.y * 256 + threadIdx.x;
+  const int turned = INTERLEAVED ? 2 * pairs / E : pairs / E;
+  int t = first / per, h = first % per / a.chunks, c = first % a.chunks;
+  while (t < nt) {
+    Piece<F32> lo[U], hi[INTERLEAVED ? 1 : U];
+    int vt[U], vh[U], vc[U];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int p = INTERLEAVED ? 2 * j : j, q = INTERLEAVED ? 2 * j + 1 : 8 + j;
-        const float u = v[p], w = v[q], co = cs[j].x, si = cs[j].y;
-        v[p] = __builtin_fmaf(u, co, -(w * si));
-        v[q] = __builtin_fmaf(w, co, u * si);
-      }
+    for (int u = 0; u < U; ++u) {
+      vt[u] = t, vh[u] = h, vc[u] = c;
+      c += a.dc, h += a.dh, t += a.dt;
+      if (c >= a.chunks) c -= a.chunks, ++h;
+      if (h >= a.heads) h -= a.heads, ++t;
     }
-    store16<F32>(y + lo, y + hi, v);
+    // bytes of an item's pieces in its head; behind the pairs (halves) two side by side
+    auto at_lo = [&](int u) { return 16 * (INTERLEAVED || vc[u] < turned ? vc[u] : 2 * vc[u]); };
+    auto at_hi = [&](int u) { return 16 * (vc[u] < turned ? vc[u] + turned : 2 * vc[u] + 1); };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (vt[u] < nt) {
+        const char* x = a.x + (t0 + vt[u]) * a.x_token + vh[u] * a.x_head;
+        lo[u].w = stream16(x + at_lo(u));
+        if constexpr (!INTERLEAVED) hi[u].w = stream16(x + at_hi(u));
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (vt[u] < nt) {
+        char* y = a.y + (t0 + vt[u]) * a.y_token + vh[u] * a.y_head;
+        const float2* cs = rot + vt[u] * pairs + vc[u] * (INTERLEAVED ? E / 2 : E);
+        if constexpr (INTERLEAVED) {
+          if (vc[u] < turned) turn_beside(lo[u], cs);
+        } else {
+          if (vc[u] < turned) turn_halves(lo[u], hi[u], cs);
+          *(u32x4*)(y + at_hi(u)) = hi[u].w;
+        }
+        *(u32x4*)(y + at_lo(u)) = lo[u].w;
+      }
   }
 }
 
@@ -213,44 +241,52 @@ struct AppendArgs {
   long k_token, k_head, v_token, v_head, q_token, q_head, o_token, o_head;   // bytes
   Batch b;
   int heads, heads_q, tt, rotate;
+  int log_tt;
   RotArgs rot;
 };
 
-// Eight consecutive values of a turned row: value j of chunk c, with its
-// partner from `other` (the other half of the pair, or the value beside it).
-__device__ __forceinline__ void turn8(float* v, const char* row, int c, const RotArgs& r, const float2* cs) {
-  const int pairs = r.pairs;
-  if (8 * c >= 2 * pairs) return;
+// Eight consecutive values (chunk c) of a turned row; for halves, o holds the
+// chunk of their partners.
+__device__ __forceinline__ u32x4 turn8(u32x4 w, u32x4 o, int c, const RotArgs& r, const float2* cs) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[2 * j] = bf16_lo(w[j]), v[2 * j + 1] = bf16_hi(w[j]);
   if (r.interleaved) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float2 z = cs[4 * c + j];
-      const float u = v[2 * j], w = v[2 * j + 1];
-      v[2 * j] = __builtin_fmaf(u, z.x, -(w * z.y));
-      v[2 * j + 1] = __builtin_fmaf(w, z.x, u * z.y);
+      const float x = v[2 * j], y = v[2 * j + 1];
+      w[j] = pack_bf16(__builtin_fmaf(x, z.x, -(y * z.y)), __builtin_fmaf(y, z.x, x * z.y));
     }
-    return;
+    return w;
   }
-  const bool low = 8 * c < pairs;
-  const u32x4 o = *(const u32x4*)(row + 2 * (low ? 8 * c + pairs : 8 * c - pairs));
-  const float2* z = cs + (low ? 8 * c : 8 * c - pairs);
+  const bool low = 8 * c < r.pairs;
+  const float2* z = cs + (low ? 8 * c : 8 * c - r.pairs);
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const float w = (j & 1) ? bf16_hi(o[j / 2]) : bf16_lo(o[j / 2]);
-    v[j] = low ? __builtin_fmaf(v[j], z[j].x, -(w * z[j].y)) : __builtin_fmaf(v[j], z[j].x, w * z[j].y);
+    const float y = (j & 1) ? bf16_hi(o[j / 2]) : bf16_lo(o[j / 2]);
+    v[j] = low ? __builtin_fmaf(v[j], z[j].x, -(y * z[j].y)) : __builtin_fmaf(v[j], z[j].x, y * z[j].y);
   }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+  return w;
 }
 
 // One thread holds 8 consecutive values of a row, D / 8 threads a row, so a
-// 32-value block of MXFP8 is four neighbouring lanes, as in mxfp8_block.  A
-// turned row takes its pairs' other halves from L1.  In place (q_out = q) a
-// row's loads all precede its stores: the row belongs to one instruction of
-// one wave.
-template <int D, bool F8>
+// 32-value block of MXFP8 is four neighbouring lanes, as in mxfp8_block, and the
+// other halves of a turned row's pairs are in its lanes.  A workgroup's tokens
+// are walked through head by head, since a page holds a head's tokens side by
+// side: 13000 tokens (32/8 heads, D 128) into MXFP8 pages 78 -> 60 us.
+// In place (q_out = q) a row's loads precede its stores: the row belongs to one
+// instruction of one wave.
+// With several tokens to a workgroup (MANY) a thread has four rows on their way
+// at once and loads past the caches; few tokens, whose rows were written just
+// before, are taken from them: 2000 tokens into bf16 pages 12.8 us, 17.6 as many.
+template <int D, bool F8, bool MANY>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   extern __shared__ float2 rot[];          // [tt][pairs]
   __shared__ long slot[kRopeTokens];       // row of head 0 in the cache, -1: none
-  constexpr int C = D / 8;
+  constexpr int C = D / 8, U = MANY ? 4 : 1;
   const long t0 = (long)blockIdx.x * a.tt;
   const int nt = (int)min((long)a.tt, a.b.tokens - t0);
   const int wave = threadIdx.x >> 6;
@@ -274,51 +310,68 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   for (int i = threadIdx.x; i < nt * pairs; i += 256)
     rot[i] = rot_of(a.rot, t0 + i / pairs, i % pairs, false);
   __syncthreads();
-  const int rows = 2 * a.heads + a.heads_q;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < nt * rows * C; i += 256 * gridDim.y) {
-    const int t = i / (rows * C), r = i % (rows * C) / C, c = i % C;
-    const long s = slot[t];
-    const bool is_q = r >= 2 * a.heads, is_v = !is_q && r >= a.heads;
-    if (is_q ? s == -2 : s < 0) continue;  // whole rows
-    const int h = is_q ? r - 2 * a.heads : is_v ? r - a.heads : r;
-    const char* row = is_q ? a.q + (t0 + t) * a.q_token + h * a.q_head
-                    : is_v ? a.v + (t0 + t) * a.v_token + h * a.v_head
-                           : a.k + (t0 + t) * a.k_token + h * a.k_head;
-    u32x4 w = *(const u32x4*)(row + 16 * c);
-    if (!is_v && pairs) {
-      float v[8];
+  const int total = (2 * a.heads + a.heads_q) << a.log_tt, c = threadIdx.x % C;
+  const bool turned = 8 * c < 2 * pairs;
+  const int partner = (threadIdx.x & 63) - c + (8 * c < pairs ? c + pairs / 8 : c - pairs / 8);   // a lane
+  for (int i = (blockIdx.y * 256 + threadIdx.x) / C; i < total; i += U * (256 / C) * gridDim.y) {
+    u32x4 w[U];
+    int vt[U], vr[U];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[2 * j] = bf16_lo(w[j]), v[2 * j + 1] = bf16_hi(w[j]);
-      turn8(v, row, c, a.rot, rot + t * pairs);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+    for (int u = 0; u < U; ++u) {
+      const int j = i + u * (256 / C) * gridDim.y;
+      vt[u] = j < total ? j & (a.tt - 1) : a.tt, vr[u] = j >> a.log_tt;
     }
-    if (is_q) {
-      *(u32x4*)(a.qo + (t0 + t) * a.o_token + h * a.o_head + 16 * c) = w;
-      continue;
-    }
-    const long to = s + ((long)h << a.b.shift);
-    if constexpr (!F8) {
-      *(u32x4*)((is_v ? a.vc : a.kc) + to * (2 * D) + 16 * c) = w;
-    } else {
-      unsigned am = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) am = max(am, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-      am = max(am, (unsigned)__shfl_xor((int)am, 1));
-      am = max(am, (unsigned)__shfl_xor((int)am, 2));
-      const int e = (int)(am >> 7), k = e == 0 ? -127 : max(e - 135, -127);
-      typedef __attribute__((ext_vector_type(2))) short s16x2;
-      auto y = [&](float f) { return __builtin_amdgcn_fmed3f(ldexpf(f, -k), -448.0f, 448.0f); };
-      unsigned p[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        s16x2 z = {0, 0};
-        z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(w[2 * j])), y(bf16_hi(w[2 * j])), 1.0f, false);
-        z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(w[2 * j + 1])), y(bf16_hi(w[2 * j + 1])), 1.0f, true);
-        p[j] = __builtin_bit_cast(unsigned, z);
+    for (int u = 0; u < U; ++u)
+      if (vt[u] < nt) {
+        const bool is_q = vr[u] >= 2 * a.heads, is_v = !is_q && vr[u] >= a.heads;
+        const long tok = t0 + vt[u];
+        const char* row = is_q ? a.q + tok * a.q_token + (vr[u] - 2 * a.heads) * a.q_head
+                        : is_v ? a.v + tok * a.v_token + (vr[u] - a.heads) * a.v_head
+                               : a.k + tok * a.k_token + vr[u] * a.k_head;
+        w[u] = MANY ? stream16(row + 16 * c) : *(const u32x4*)(row + 16 * c);
       }
-      *(uint2*)((is_v ? a.vc : a.kc) + to * D + 8 * c) = make_uint2(p[0], p[1]);
-      if ((c & 3) == 0) (is_v ? a.vs : a.ks)[to * (D / 32) + c / 4] = (uint8_t)(k + 127);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (vt[u] >= nt) continue;           // whole rows, here and below
+      const long s = slot[vt[u]];
+      const bool is_q = vr[u] >= 2 * a.heads, is_v = !is_q && vr[u] >= a.heads;
+      if (is_q ? s == -2 : s < 0) continue;
+      u32x4 x = w[u];
+      if (pairs && !is_v) {
+        u32x4 o = x;
+        if (!a.rot.interleaved)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[j] = (unsigned)__shfl((int)x[j], partner);
+        if (turned) x = turn8(x, o, c, a.rot, rot + vt[u] * pairs);
+      }
+      if (is_q) {
+        *(u32x4*)(a.qo + (t0 + vt[u]) * a.o_token + (vr[u] - 2 * a.heads) * a.o_head + 16 * c) = x;
+        continue;
+      }
+      const long to = s + ((long)(is_v ? vr[u] - a.heads : vr[u]) << a.b.shift);
+      if constexpr (!F8) {
+        *(u32x4*)((is_v ? a.vc : a.kc) + to * (2 * D) + 16 * c) = x;
+      } else {
+        unsigned am = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) am = max(am, max(x[j] & 0x7fffu, (x[j] >> 16) & 0x7fffu));
+        am = max(am, (unsigned)__shfl_xor((int)am, 1));
+        am = max(am, (unsigned)__shfl_xor((int)am, 2));
+        const int e = (int)(am >> 7), k = e == 0 ? -127 : max(e - 135, -127);
+        typedef __attribute__((ext_vector_type(2))) short s16x2;
+        auto y = [&](float f) { return __builtin_amdgcn_fmed3f(ldexpf(f, -k), -448.0f, 448.0f); };
+        unsigned p[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          s16x2 z = {0, 0};
+          z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(x[2 * j])), y(bf16_hi(x[2 * j])), 1.0f, false);
+          z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(x[2 * j + 1])), y(bf16_hi(x[2 * j + 1])), 1.0f, true);
+          p[j] = __builtin_bit_cast(unsigned, z);
+        }
+        *(uint2*)((is_v ? a.vc : a.kc) + to * D + 8 * c) = make_uint2(p[0], p[1]);
+        if ((c & 3) == 0) (is_v ? a.vs : a.ks)[to * (D / 32) + c / 4] = (uint8_t)(k + 127);
+      }
     }
   }
 }
@@ -433,11 +486,6 @@ __device__ __forceinline__ int step_v_at(int r, int c) {
   const int f = D == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1;
   return r * (2 * D) + ((c ^ f) << 4);
 }
-
-// Keys and values are read once, so their loads ask the caches not to keep
-// them: one token over 131000 keys (32/8 heads, D 128, bf16) 99.9 -> 87.5 us
-// (5.37 -> 6.13 TB/s), 300 tokens over 1000 keys each 141 -> 131 us.
-__device__ __forceinline__ u32x4 stream16(const char* p) { return __builtin_nontemporal_load((const u32x4*)p); }
 
 // One tile in registers.  A lane has row lane % 16 of every 16-key half of K:
 // 16-byte pieces g, g + 4, .. of it (g = lane / 16), so that a load takes 64
@@ -1272,12 +1320,18 @@ Batch batch_args(const efq_batch* b, const efq_cache* c) {
                __builtin_ctz((unsigned)c->page_size)};
 }
 
-// Tokens of a workgroup and workgroups of a token in the kernels that walk
-// over tokens: few tokens are spread over the chip a workgroup per 256 threads'
-// work, many share the sines of several tokens in one workgroup.
+// Tokens of a workgroup (a power of two) and workgroups of a token in the kernels
+// that walk over tokens: few tokens are spread over the chip a workgroup per 256
+// threads' work, many share one workgroup as long as eight are left for a CU.
 void token_grid(int tokens, int threads_per_token, int& tt, int& parts) {
-  tt = std::max(1, std::min(kRopeTokens, tokens / (8 * kCUs)));
+  for (tt = kRopeTokens; tt > 1 && tokens < tt * 8 * kCUs; tt /= 2) {}
   parts = tt > 1 || tokens > 4 * kCUs ? 1 : (threads_per_token + 255) / 256;
+}
+
+template <int D, bool F8, bool MANY>
+hipError_t launch_append(const AppendArgs& a, dim3 grid, int lds, hipStream_t st) {
+  hipLaunchKernelGGL((kv_append_kernel<D, F8, MANY>), grid, dim3(256), lds, st, a);
+  return hipGetLastError();
 }
 
 // How a call's rows are cut: the kernel, its rows per workgroup, and the
@@ -1410,10 +1464,12 @@ int efq_rope(const efq_rows* x, const efq_rows* y, int tokens, int heads, int he
   a.x = (const char*)x->data;
   a.y = (char*)y->data;
   a.x_token = x->token * es, a.x_head = x->head * es, a.y_token = y->token * es, a.y_head = y->head * es;
-  a.tokens = tokens, a.heads = heads, a.chunks = head_dim / 16, a.inverse = inverse != 0;
+  a.tokens = tokens, a.heads = heads, a.chunks = head_dim * es / (rot->interleaved ? 16 : 32), a.inverse = inverse != 0;
   a.rot = rot_args(rot, tokens);
   int parts;
   token_grid(tokens, heads * a.chunks, a.tt, parts);
+  const int step = 256 * parts, per = heads * a.chunks;
+  a.dt = step / per, a.dh = step % per / a.chunks, a.dc = step % a.chunks;
   const dim3 grid((unsigned)(((long)tokens + a.tt - 1) / a.tt), (unsigned)parts);
   const int lds = a.tt * rot->pairs * (int)sizeof(float2);
   hipStream_t st = (hipStream_t)stream;
@@ -1454,16 +1510,18 @@ int efq_kv_append(const efq_rows* k, const efq_rows* v, const efq_cache* cache, 
   a.heads = cache->heads_kv, a.heads_q = heads_q;
   if (rot) a.rotate = 1, a.rot = rot_args(rot, batch->tokens);
   int parts;
-  token_grid(batch->tokens, (2 * a.heads + heads_q) * (D / 8), a.tt, parts);
+  const int rows = 2 * a.heads + heads_q;
+  token_grid(batch->tokens, rows * (D / 8), a.tt, parts);
+  a.log_tt = __builtin_ctz((unsigned)a.tt);
   const dim3 grid((unsigned)(((long)batch->tokens + a.tt - 1) / a.tt), (unsigned)parts);
   const int lds = rot ? a.tt * rot->pairs * (int)sizeof(float2) : 0;
   hipStream_t st = (hipStream_t)stream;
   const bool f8 = cache->format == EFQ_CACHE_MXFP8;
-  if (D == 128 && f8) hipLaunchKernelGGL((kv_append_kernel<128, true>), grid, dim3(256), lds, st, a);
-  else if (D == 128) hipLaunchKernelGGL((kv_append_kernel<128, false>), grid, dim3(256), lds, st, a);
-  else if (f8) hipLaunchKernelGGL((kv_append_kernel<64, true>), grid, dim3(256), lds, st, a);
-  else hipLaunchKernelGGL((kv_append_kernel<64, false>), grid, dim3(256), lds, st, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (a.tt > 1) e = D == 128 ? (f8 ? launch_append<128, true, true>(a, grid, lds, st) : launch_append<128, false, true>(a, grid, lds, st))
+                             : (f8 ? launch_append<64, true, true>(a, grid, lds, st) : launch_append<64, false, true>(a, grid, lds, st));
+  else e = D == 128 ? (f8 ? launch_append<128, true, false>(a, grid, lds, st) : launch_append<128, false, false>(a, grid, lds, st))
+                    : (f8 ? launch_append<64, true, false>(a, grid, lds, st) : launch_append<64, false, false>(a, grid, lds, st));
   if (e != hipSuccess) return fail(EFQ_EHIP, "append launch: %s", hipGetErrorString(e));
   return EFQ_OK;
 }
