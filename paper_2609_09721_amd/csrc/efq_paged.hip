@@ -827,7 +827,7 @@ template <int D, bool F8, int NW>
 struct ChunkFeed {
   static constexpr int RB = F8 ? D : 2 * D;                 // bytes of a row
   static constexpr int RI = 1024 / RB;                      // rows of a piece
-  static constexpr int PER = kBc / RI > NW ? kBc / RI / NW : 1;   // pieces of a wave
+  static constexpr int PER = kBc / RI / NW;                 // pieces of a wave
   long at[2][PER];                                          // cache row of a piece: of K's tile, of the tile before
   int rows[2][PER];                                         // rows of it that are keys
   u32x4 kc[F8 ? PER : 1], vc[F8 ? PER : 1];                 // MXFP8: codes and scales on their way
@@ -845,13 +845,13 @@ struct ChunkFeed {
     return is_v ? chunk_v_swz<D>(N * RI) << 4 : chunk_k_swz<D>(N * RI) << 4;
   }
   __device__ __forceinline__ static int first_row(int wave, int n) { return (F8 ? wave + n * NW : wave * PER + n) * RI; }
-  static constexpr bool kHalf = kBc / RI < NW;              // only some waves have a piece
+  static_assert(kBc / RI == PER * NW, "every wave has PER pieces");
 
   // ids: lane 4 (tile % 16) + quarter has the page of that 16-key quarter
   template <int N>
   __device__ __forceinline__ void place(const PagedArgs& a, int h, int ids, int tile, int key0, int k1, int wave) {
     const int r0 = first_row(wave, N);
-    const int id = __builtin_amdgcn_readlane(ids, (4 * (tile & 15) + r0 / 16) & 63);
+    const int id = __builtin_amdgcn_readlane(ids, 4 * (tile & 15) + r0 / 16);
     const bool ok = (unsigned)id < (unsigned)a.b.pages;
     at[1][N] = at[0][N];
     rows[1][N] = rows[0][N];
@@ -871,7 +871,7 @@ struct ChunkFeed {
       c = u32x4{0u, 0u, 0u, 0u};
       e = 0u;
       const int r = lane * RI / 64;
-      if (r < rows[V][N] && (!kHalf || wave * RI < kBc)) {
+      if (r < rows[V][N]) {
         c = *(const u32x4*)(base + at[V][N] * RB + (unsigned)(16 * lane));
         e = ((V ? a.vs : a.ks) + at[V][N] * (D / 32))[(unsigned)(r * (D / 32) + lane % (64 / RI) / 2)];
       }
@@ -881,7 +881,6 @@ struct ChunkFeed {
   template <int N, int V>
   __device__ __forceinline__ void land(uint8_t* to, int wave, int lane) {
     const int r = first_row(wave, N) + lane * RI / 64, c = lane % (64 / RI);
-    if (kHalf && wave * RI >= kBc) return;
     const int swz = V ? chunk_v_swz<D>(r) : chunk_k_swz<D>(r);
     const u32x4& x = V ? vc[N] : kc[N];
     const float sc = e8m0_scale(V ? ve[N] : ke[N]);
@@ -1363,7 +1362,8 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
     // Splits of the longest sequence: as many as put two workgroups on every
     // CU; sequences of different lengths (more than one) also want pieces small
     // enough to end together, down to 448 KB of keys and values, which stream in
-    // about ten times what it takes to start a workgroup.  17 sequences of 5000
+    // about ten times what it takes to start a workgroup, while the unsplit call
+    // has fewer than eight rounds of workgroups.  17 sequences of 5000
     // to 20000 keys (32/8 heads, D 128, bf16) in pieces of 6700 / 2900 / 1540 /
     // 830 keys: 164 / 171 / 145 / 138 us; one of 131000 keys in 64 / 256 pieces
     // 87 / 98 us.  Below 1024 keys the join costs more than it saves (one
@@ -1372,7 +1372,7 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
     const long items = std::max<long>(1, p.slots * c->heads_kv);
     const long key_bytes = 2 * (low ? c->head_dim + c->head_dim / 32 : 2 * c->head_dim);
     n = (2 * kCUs + items - 1) / items;
-    if (b->seqs > 1) n = std::max(n, keys * key_bytes / (448 << 10));
+    if (b->seqs > 1) n = std::max(n, std::min(keys * key_bytes / (448 << 10), 16 * kCUs / items));
     n = keys < 1024 ? 1 : std::max<long>(1, std::min(n, keys / 256));
   } else {
     // As many pieces (of at least 256 keys) as leave the chip one round of
@@ -1383,6 +1383,7 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
     const long items = b->seqs * (((long)b->tokens * G / b->seqs + p.bm - 1) / p.bm) * c->heads_kv;
     n = std::max<long>(1, std::min((kCUs + (b->seqs > 1 ? items / 2 : 0)) / std::max<long>(1, items), keys / 256));
   }
+  n = std::min<long>(n, 4096);             // within a grid's second dimension
   p.chunk = (int)(((keys + n - 1) / n + 127) / 128 * 128);
   p.nsplit = (int)std::max<long>(1, (keys + p.chunk - 1) / p.chunk);
   p.bytes = p.nsplit == 1 ? 0 : round256((size_t)p.nsplit * b->tokens * heads_q * 8) +
