@@ -802,85 +802,115 @@ __device__ __forceinline__ int chunk_k_swz(int r) { return D == 128 ? r & 15 : (
 template <int D>
 __device__ __forceinline__ int chunk_v_swz(int r) { return D == 128 ? ((r & 3) << 2) ^ (r & 2) : ((r >> 1) & 1) << 2; }
 
-// One 1 KB direct-to-LDS load: lane i's 16 bytes at `from` + voff land at LDS
-// address `to` + 16 i, zeros where voff is past `bytes`.  In assembly, since
+// One 1 KB direct-to-LDS load through a buffer resource (address, bytes): lane
+// i's 16 bytes at voff land at LDS address `to` + 16 i, zeros where voff is past
+// the resource's bytes.  In assembly, since
 // the compiler would wait for all such loads before the next transposing read;
 // it has no register output, and the kernel's own waits count it.  Waits that
 // the compiler places for its loads count it too, and so only wait longer.
-__device__ __forceinline__ void load_lds_1k(const char* from, int bytes, unsigned to, int voff) {
-  const unsigned long long p = (unsigned long long)from;
-  const u32x4 rsrc = {(unsigned)p, (unsigned)(p >> 32) & 0xffffu, (unsigned)bytes, 0x00020000u};
+__device__ __forceinline__ void load_lds_1k(u32x4 rsrc, unsigned to, int voff) {
   // (five wait states from a vector instruction that writes a scalar register to
   // a memory instruction that reads it, one from the write of m0, which the
   // compiler sets anew before any instruction of its own that reads it)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :: "s"(to), "v"(voff), "s"(rsrc) : "memory");
 }
+// 16 bytes, one byte at `from` + voff, zero where voff is past `bytes`.
+__device__ __forceinline__ u32x4 raw_load16(const char* from, unsigned bytes, int voff) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(from, bytes), voff, 0, 0));
+}
+__device__ __forceinline__ unsigned raw_load1(const char* from, unsigned bytes, int voff) {
+  return (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(make_rsrc(from, bytes), voff, 0, 0);
+}
 
 // A kernel's lambdas that hold its registers by reference have to be inlined.
 #define EFQ_INLINE __attribute__((always_inline))
 
-// What brings the K and V tiles of one slot into LDS.  A tile's rows come in
-// pieces, one per load of a wave: where they lie is worked out for K and used
-// again for V, which follows a tile behind.
+// What brings the K and V tiles of one slot into LDS.  A wave brings the same 8
+// or 16 rows of every tile, which lie in one page.  Where they lie is worked out
+// for 64 tiles at once, lane t for tile t of a group, so that a step only reads
+// it out of the lane; the pages of the next group are asked for meanwhile.
 template <int D, bool F8, int NW>
 struct ChunkFeed {
   static constexpr int RB = F8 ? D : 2 * D;                 // bytes of a row
-  static constexpr int RI = 1024 / RB;                      // rows of a piece
-  static constexpr int PER = kBc / RI / NW;                 // pieces of a wave
-  long at[2][PER];                                          // cache row of a piece: of K's tile, of the tile before
-  int rows[2][PER];                                         // rows of it that are keys
+  static constexpr int ROWS = kBc / NW;                     // rows of a wave
+  static constexpr int PER = ROWS * RB / 1024;              // its 1 KB loads of K, and of V
+  static_assert(PER * 1024 == ROWS * RB && 16 % ROWS == 0, "a wave's rows are whole loads in one page");
+  static constexpr int RI = ROWS / PER;                     // rows of a load
+  // Of the group's tiles: address of K and V (MXFP8: cache row, in k), bytes of
+  // the wave's rows that are keys (MXFP8: rows), a bit for each 16-key quarter
+  // whose page is none (and 4 bits up, of the group before).
+  unsigned klo, khi, vlo, vhi, n, none;
+  unsigned v_lo, v_hi, v_n;                                 // of the tile before: V follows K by a tile
   u32x4 kc[F8 ? PER : 1], vc[F8 ? PER : 1];                 // MXFP8: codes and scales on their way
   unsigned ke[F8 ? PER : 1], ve[F8 ? PER : 1];
-  int off[2];                                               // bf16: the lane's place in a piece of K, of V
+  int off[2];                                               // the lane's place in a load of K, of V
 
   __device__ __forceinline__ void init(int wave, int lane) {
-    const int r = wave * PER * RI + lane * RI / 64, c = lane % (64 / RI);
-    off[0] = (lane * RI / 64) * RB + ((c ^ chunk_k_swz<D>(r)) << 4);
-    off[1] = (lane * RI / 64) * RB + ((c ^ chunk_v_swz<D>(r)) << 4);
+    const int r = wave * ROWS + lane * RI / 64, c = lane % (64 / RI);
+    off[0] = F8 ? 16 * lane : (lane * RI / 64) * RB + ((c ^ chunk_k_swz<D>(r)) << 4);
+    off[1] = F8 ? 16 * lane : (lane * RI / 64) * RB + ((c ^ chunk_v_swz<D>(r)) << 4);
   }
-  // the swizzle of piece n against piece 0's: a bit of the row that n sets
-  template <int N>
-  static constexpr int turn(bool is_v) {
-    return is_v ? chunk_v_swz<D>(N * RI) << 4 : chunk_k_swz<D>(N * RI) << 4;
-  }
-  __device__ __forceinline__ static int first_row(int wave, int n) { return (F8 ? wave + n * NW : wave * PER + n) * RI; }
-  static_assert(kBc / RI == PER * NW, "every wave has PER pieces");
-
-  // ids: lane 4 (tile % 16) + quarter has the page of that 16-key quarter
-  template <int N>
-  __device__ __forceinline__ void place(const PagedArgs& a, int h, int ids, int tile, int key0, int k1, int wave) {
-    const int r0 = first_row(wave, N);
-    const int id = __builtin_amdgcn_readlane(ids, 4 * (tile & 15) + r0 / 16);
-    const bool ok = (unsigned)id < (unsigned)a.b.pages;
-    at[1][N] = at[0][N];
-    rows[1][N] = rows[0][N];
-    const long p = (((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)(key0 + r0) & ((1u << a.b.shift) - 1));
-    at[0][N] = (long)((unsigned long long)(unsigned)uniform((int)(p >> 32)) << 32 | (unsigned)uniform((int)p));
-    rows[0][N] = uniform(ok ? min(max(k1 - key0 - r0, 0), RI) : 0);
-  }
-  // K (V = 0) or V (1) piece N of the tile that place (the one before) worked out
+  // the place in load n against load 0's: further rows, and the swizzle's bits
+  // that they set
   template <int N, int V>
-  __device__ __forceinline__ void ask(const PagedArgs& a, const uint8_t* to, int wave, int lane) {
-    const char* base = V ? a.vc : a.kc;
-    if constexpr (!F8) {
-      load_lds_1k(base + at[V][N] * RB, rows[V][N] * RB, lds_addr(to) + (wave * PER + N) * 1024, off[V] ^ turn<N>(V));
+  __device__ __forceinline__ int place() const {
+    const int swz = V ? chunk_v_swz<D>(N * RI) : chunk_k_swz<D>(N * RI);
+    return (off[V] ^ (F8 ? 0 : swz << 4)) + N * 1024;
+  }
+
+  // (the group's pages are waited for: a microsecond in the 64 tiles' hundred)
+  __device__ __forceinline__ void take_pages(const PagedArgs& a, const int32_t* table, int h, int k0, int k1, int tile0,
+                                             int wave, int lane) {
+    none <<= 4;
+    int id = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long at = (long)k0 + (long)kBc * (tile0 + lane) + 16 * i;
+      const int page = at < k1 ? table[at >> a.b.shift] : 0;
+      if ((unsigned)page >= (unsigned)a.b.pages) none |= 1u << i;
+      if (wave * ROWS / 16 == i) id = page;
+    }
+    const bool ok = (unsigned)id < (unsigned)a.b.pages;
+    const long key = (long)k0 + (long)kBc * (tile0 + lane) + wave * ROWS;
+    const long row = (((long)(ok ? id : 0) * a.Hkv + h) << a.b.shift) + ((unsigned)key & ((1u << a.b.shift) - 1));
+    const int live = ok ? (int)min(max((long)k1 - key, 0L), (long)ROWS) : 0;
+    if constexpr (F8) {
+      klo = (unsigned)row, khi = (unsigned)(row >> 32), n = live;
     } else {
+      const unsigned long long k = (unsigned long long)(a.kc + row * RB), v = (unsigned long long)(a.vc + row * RB);
+      klo = (unsigned)k, khi = (unsigned)(k >> 32) & 0xffffu, vlo = (unsigned)v, vhi = (unsigned)(v >> 32) & 0xffffu;
+      n = live * RB;
+    }
+  }
+  // K of tile t is next, V of the tile before it
+  __device__ __forceinline__ void next_tile(int t, unsigned& lo, unsigned& hi, unsigned& bytes) {
+    lo = __builtin_amdgcn_readlane(klo, t & 63);
+    hi = __builtin_amdgcn_readlane(khi, t & 63);
+    bytes = __builtin_amdgcn_readlane(n, t & 63);
+  }
+  __device__ __forceinline__ void keep_v(int t, unsigned lo, unsigned hi, unsigned bytes) {
+    v_lo = F8 ? lo : __builtin_amdgcn_readlane(vlo, t & 63);
+    v_hi = F8 ? hi : __builtin_amdgcn_readlane(vhi, t & 63);
+    v_n = bytes;
+  }
+  template <int N, int V>
+  __device__ __forceinline__ void ask(const PagedArgs& a, unsigned lo, unsigned hi, unsigned bytes, unsigned to, int lane) {
+    if constexpr (!F8) {
+      load_lds_1k(u32x4{lo, hi, bytes, 0x00020000u}, to + N * 1024, place<N, V>());
+    } else {
+      const unsigned long long row = (unsigned long long)hi << 32 | lo;
       u32x4& c = V ? vc[N] : kc[N];
       unsigned& e = V ? ve[N] : ke[N];
-      c = u32x4{0u, 0u, 0u, 0u};
-      e = 0u;
-      const int r = lane * RI / 64;
-      if (r < rows[V][N]) {
-        c = *(const u32x4*)(base + at[V][N] * RB + (unsigned)(16 * lane));
-        e = ((V ? a.vs : a.ks) + at[V][N] * (D / 32))[(unsigned)(r * (D / 32) + lane % (64 / RI) / 2)];
-      }
+      c = raw_load16((V ? a.vc : a.kc) + row * RB, bytes * RB, place<N, V>());
+      e = raw_load1((const char*)((V ? a.vs : a.ks) + row * (D / 32)), bytes * (D / 32),
+                    (lane * RI / 64 + N * RI) * (D / 32) + lane % (64 / RI) / 2);
     }
   }
   // MXFP8: what has come, as bf16, into the tile
   template <int N, int V>
   __device__ __forceinline__ void land(uint8_t* to, int wave, int lane) {
-    const int r = first_row(wave, N) + lane * RI / 64, c = lane % (64 / RI);
+    const int r = wave * ROWS + N * RI + lane * RI / 64, c = lane % (64 / RI);
     const int swz = V ? chunk_v_swz<D>(r) : chunk_k_swz<D>(r);
     const u32x4& x = V ? vc[N] : kc[N];
     const float sc = e8m0_scale(V ? ve[N] : ke[N]);
@@ -891,11 +921,12 @@ struct ChunkFeed {
   }
 };
 
-// The running reference of a row is its maximum, but for growth below 2^8: a
-// tile's probabilities may reach 2^8 before O and the sum are rescaled, which
-// costs no precision (their rounding is relative) and leaves out almost every
-// rescaling after the first tiles.
-constexpr float kGrowth = 8.0f;
+// The running reference of a row need not be its maximum: it moves only when a
+// lane's probabilities of a tile sum up to more than this, so almost never
+// after the first tile, and until then no maximum is taken and nothing rescaled.
+// It costs no precision (the probabilities' rounding is relative, the sums are
+// fp32 and stay far below their range).
+constexpr float kMostSum = 65536.0f;
 
 // One slot's rows, split sp of their keys.
 template <int D, bool F8, int NW>
@@ -928,151 +959,116 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
   for (int i = 0; i < DT; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.0f;
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l = 0.0f, ref = 0.0f;                // ref: m, or 0 while no key was seen
 
-  const int32_t* table = a.b.table + (long)s.seq * a.b.width;
-  auto pages_from = [&](int tile) {
-    const long key = (long)k0 + (long)kBc * (tile + (lane >> 2)) + 16 * (lane & 3);
-    return key < k1 ? table[key >> a.b.shift] : 0;
-  };
-  auto bad_of = [&](int ids) { return __builtin_amdgcn_ballot_w64((unsigned)ids >= (unsigned)a.b.pages); };
-
-  typedef ChunkFeed<D, F8, NW> Feed;
-  Feed feed;
-  feed.init(wave, lane);
-  auto k_tile = [&](int t) { return lds + (t % NB) * kTile; };
-  auto v_tile = [&](int t) { return lds + (NB + t % NB) * kTile; };
-
-  // offsets of the operands in a tile: K column chunk i, V head-dim tile i
+  // LDS addresses of the operands in place 0 of the rings: K column chunk i, V
+  // head-dim tile i; and of what the wave brings
   const unsigned lds0 = lds_addr(lds);
   unsigned ka[KK], va[DT];
 #pragma unroll
-  for (int i = 0; i < KK; ++i) ka[i] = col * 2 * D + (((2 * i + half) ^ chunk_k_swz<D>(col)) << 4);
+  for (int i = 0; i < KK; ++i) ka[i] = lds0 + col * 2 * D + (((2 * i + half) ^ chunk_k_swz<D>(col)) << 4);
   {
     const int vr = 4 * half + ((lane & 15) >> 2);
 #pragma unroll
     for (int i = 0; i < DT; ++i) {
       const int c = 4 * i + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-      va[i] = vr * 2 * D + ((c ^ chunk_v_swz<D>(vr)) << 4) + 8 * (lane & 1);
+      va[i] = lds0 + NB * kTile + vr * 2 * D + ((c ^ chunk_v_swz<D>(vr)) << 4) + 8 * (lane & 1);
     }
   }
 
-  // Pages of tiles 16 grp .. 16 grp + 15 (ids) and of the next 16 (next), with
-  // a bit for each quarter whose page is none; j's group is grp.
-  // They are asked for 8 tiles before they are taken over, in a register of
-  // their own, so that only the taking over waits for them.
-  int ids = 0, next = 0, asked = 0, grp = 0;
-  unsigned long long bad = 0, next_bad = 0;
-  auto turn_page = [&](int j) EFQ_INLINE {
-    if ((j & 15) == 8) {
-      next = asked;
-      next_bad = bad_of(next);
-    }
-    if ((j & 15) == 0 && j > 0) {
-      ids = next;
-      bad = next_bad;
-      asked = pages_from(j + 16);
-      ++grp;
-    }
+  // Step j brings K tile t = j + NB and V tile t - 1, a load (of K, then of V)
+  // at a time.  Past the last tile the loads go on, of no bytes, so that a wait
+  // counts the same loads in every step.  t is in ring place SLOT, j too.
+  typedef ChunkFeed<D, F8, NW> Feed;
+  Feed feed;
+  feed.init(wave, lane);
+  feed.none = feed.v_n = feed.v_lo = feed.v_hi = 0u;
+  const int32_t* table = a.b.table + (long)s.seq * a.b.width;
+  const unsigned brings = lds0 + wave * (Feed::PER * 1024);
+  unsigned f_lo, f_hi, f_n;                                 // K's place in the step's fetch
+  auto turn_page = [&](int t) EFQ_INLINE {
+    if ((t & 63) == 0) feed.take_pages(a, table, h, k0, k1, t, wave, lane);
   };
-  // Piece I of what a step brings: K tile t (the first PER), V tile t - 1.
-  // Past the last tile the loads go on, of no bytes, so that a wait counts the
-  // same loads in every step.
-  auto fetch_one = [&](auto piece, int t) EFQ_INLINE {
-    constexpr int I = decltype(piece)::value;
+  auto fetch_one = [&](auto slot, auto piece, int t) EFQ_INLINE {
+    constexpr int SLOT = decltype(slot)::value, I = decltype(piece)::value;
+    if constexpr (I == 0) feed.next_tile(t, f_lo, f_hi, f_n);
     if constexpr (I < Feed::PER) {
-      feed.template place<I>(a, h, t >> 4 == grp ? ids : next, t, k0 + kBc * t, k1, wave);
-      feed.template ask<I, 0>(a, k_tile(t), wave, lane);
+      feed.template ask<I, 0>(a, f_lo, f_hi, f_n, brings + SLOT * kTile, lane);
     } else {
-      feed.template ask<I - Feed::PER, 1>(a, v_tile(t - 1), wave, lane);
+      feed.template ask<I - Feed::PER, 1>(a, feed.v_lo, feed.v_hi, feed.v_n, brings + (NB + (SLOT + NB - 1) % NB) * kTile, lane);
+      if constexpr (I == 2 * Feed::PER - 1) feed.keep_v(t, f_lo, f_hi, f_n);
     }
   };
-  auto fetch_k = [&](int t) EFQ_INLINE { static_for<Feed::PER>([&](auto i) EFQ_INLINE { fetch_one(i, t); }); };
-  auto fetch = [&](int t) EFQ_INLINE { static_for<2 * Feed::PER>([&](auto i) EFQ_INLINE { fetch_one(i, t); }); };
-  auto land_k = [&](int t) EFQ_INLINE {
-    if constexpr (F8)
-      static_for<Feed::PER>([&](auto i) EFQ_INLINE { feed.template land<decltype(i)::value, 0>(k_tile(t), wave, lane); });
+  auto fetch = [&](auto slot, int t) EFQ_INLINE {
+    static_for<2 * Feed::PER>([&](auto i) EFQ_INLINE { fetch_one(slot, i, t); });
   };
-  auto land = [&](int t) EFQ_INLINE {                       // K tile t, V tile t - 1
+  auto land = [&](auto slot) EFQ_INLINE {                   // the K tile of place SLOT, the V tile of the one before
+    constexpr int SLOT = decltype(slot)::value;
     if constexpr (F8) {
-      land_k(t);
-      static_for<Feed::PER>([&](auto i) EFQ_INLINE { feed.template land<decltype(i)::value, 1>(v_tile(t - 1), wave, lane); });
+      static_for<Feed::PER>([&](auto i) EFQ_INLINE {
+        feed.template land<decltype(i)::value, 0>(lds + SLOT * kTile, wave, lane);
+        feed.template land<decltype(i)::value, 1>(lds + (NB + (SLOT + NB - 1) % NB) * kTile, wave, lane);
+      });
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
   };
 
   f32x16 sc[2];
   bf16x8 p[4];
-  auto scores = [&](int t) EFQ_INLINE {
-    const unsigned kt = lds0 + t % NB * kTile;
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[w][i] = 0.0f;
-#pragma unroll
-      for (int i = 0; i < KK; ++i) {
-        const bf16x8 kop = *(__attribute__((address_space(3))) const bf16x8*)(lds_at(kt + ka[i]) + w * 64 * D);
-        sc[w] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kop, q[i], sc[w], 0, 0, 0);
-      }
-    }
-  };
   // M(j) is NV products of V tile j with its probabilities, then NK of K tile
-  // j + 1 with Q.  Their operands are read kAhead products before they are used
-  // (an LDS read takes as long as about four products), the first ones at the
-  // end of the vector phase before.
+  // j + 1 with Q, in pairs whose second operand is read first, so that one wait
+  // serves both.  Operands are read kAhead products before they are used (an LDS
+  // read takes as long as about four), the first ones at the end of the vector
+  // phase before.  A wave issues an instruction in five cycles at best and a
+  // product takes 32: what stands between two products is counted.
   constexpr int NV = 4 * DT, NK = 2 * KK, kAhead = 4;
   bf16x8 op[NV + NK];
-  auto read_op = [&](auto n, unsigned kt, unsigned vt) EFQ_INLINE {
-    constexpr int N = decltype(n)::value;
+  auto read_op = [&](auto slot, auto n) EFQ_INLINE {        // slot: of tile j
+    constexpr int SLOT = decltype(slot)::value, N = decltype(n)::value;
     if constexpr (N < NV) {
-      const lds_cptr at = lds_at(vt + va[N % DT]) + (N / DT) * 32 * D;
+      const lds_cptr at = lds_at(va[N % DT]) + SLOT * kTile + (N / DT) * 32 * D;
       const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
       const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * D));
       op[N] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     } else if constexpr (N < NV + NK) {
       constexpr int I = N - NV;
-      op[N] = *(__attribute__((address_space(3))) const bf16x8*)(lds_at(kt + ka[I / 2]) + (I % 2) * 64 * D);
+      op[N] = *(__attribute__((address_space(3))) const bf16x8*)(lds_at(ka[I / 2]) + (SLOT + 1) % NB * kTile + (I % 2) * 64 * D);
     }
   };
-  auto tiles_at = [&](int j, unsigned& kt, unsigned& vt) EFQ_INLINE {
-    kt = lds0 + (j + 1) % NB * kTile;
-    vt = lds0 + (NB + j % NB) * kTile;
-  };
-  auto first_ops = [&](int j) EFQ_INLINE {
-    unsigned kt, vt;
-    tiles_at(j, kt, vt);
-    static_for<kAhead>([&](auto n) EFQ_INLINE { read_op(n, kt, vt); });
-  };
-  // The step's loads are asked for between products, in whose shadow the scalar
-  // work of finding their addresses costs nothing.
-  auto phase_m = [&](int j) EFQ_INLINE {
-    if (j >= mine) return fetch(j + NB);
-    __builtin_amdgcn_s_setprio(1);
-    unsigned kt, vt;
-    tiles_at(j, kt, vt);
-    static_for<NV + NK>([&](auto n) EFQ_INLINE {
-      constexpr int N = decltype(n)::value;
-      if constexpr (N < NV) {
-        o[N % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[N], p[N / DT], o[N % DT], 0, 0, 0);
-      } else {
-        constexpr int I = N - NV, W = I % 2;
-        if constexpr (I < 2) {
+  auto product = [&](auto n) EFQ_INLINE {
+    constexpr int N = decltype(n)::value;
+    if constexpr (N < NV) {
+      o[N % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[N], p[N / DT], o[N % DT], 0, 0, 0);
+    } else {
+      constexpr int I = N - NV, W = I % 2;
+      if constexpr (I < 2) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sc[W][i] = 0.0f;
-        }
-        sc[W] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[N], q[I / 2], sc[W], 0, 0, 0);
+        for (int i = 0; i < 16; ++i) sc[W][i] = 0.0f;
       }
-      read_op(std::integral_constant<int, N + kAhead>{}, kt, vt);
-      constexpr int kEvery = (NV + NK) / (2 * Feed::PER);
-      if constexpr (N % kEvery == kEvery / 2) fetch_one(std::integral_constant<int, N / kEvery>{}, j + NB);
+      sc[W] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(op[N], q[I / 2], sc[W], 0, 0, 0);
+    }
+  };
+  auto phase_m = [&](auto slot, int j) EFQ_INLINE {
+    if (j >= mine) return fetch(slot, j + NB);
+    __builtin_amdgcn_s_setprio(1);
+    static_for<(NV + NK) / 2>([&](auto n) EFQ_INLINE {
+      constexpr int N = 2 * decltype(n)::value, kEvery = (NV + NK) / (2 * Feed::PER);
+      product(std::integral_constant<int, N + 1>{});
+      read_op(slot, std::integral_constant<int, N + kAhead>{});
+      __builtin_amdgcn_sched_barrier(0);
+      product(std::integral_constant<int, N>{});
+      read_op(slot, std::integral_constant<int, N + kAhead + 1>{});
+      // the step's loads, in the products' shadow
+      if constexpr (N % kEvery == kEvery / 2) fetch_one(slot, std::integral_constant<int, N / kEvery>{}, j + NB);
       __builtin_amdgcn_sched_barrier(0);
     });
   };
-  auto phase_v = [&](int j) EFQ_INLINE {                    // probabilities of tile j
+  auto phase_v = [&](auto slot, int j) EFQ_INLINE {         // probabilities of tile j, in place SLOT
     if (j >= mine) return;
     __builtin_amdgcn_s_setprio(0);
     const int key0 = k0 + kBc * j;
-    const unsigned none = (unsigned)((j >> 4 == grp ? bad : next_bad) >> (4 * (j & 15))) & 15u;
+    // (the feed's group is that of tile j + NB - 1)
+    const unsigned none = (unsigned)__builtin_amdgcn_readlane(feed.none, j & 63) >> ((j & 63) > 64 - NB ? 4 : 0) & 15u;
     if (none || key0 + kBc > free_of_mask) {
 #pragma unroll
       for (int w = 0; w < 2; ++w)
@@ -1082,70 +1078,86 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
           if (key0 + kw >= vis || (none >> (2 * w + (i >> 3)) & 1)) sc[w][i] = -INFINITY;
         }
     }
-    const float mx = max_of_halves(__builtin_fmaxf(max16(sc[0]), max16(sc[1]))) * a.sl2;
-    if (__builtin_amdgcn_ballot_w64(mx > m + kGrowth)) {
+    u32x4 pw[4];
+    float sum;
+    auto probabilities = [&]() EFQ_INLINE {
+      float part[4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        part[ks] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16& x = sc[ks / 2];
+          const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[8 * (ks & 1) + 2 * i], a.sl2, -ref));
+          const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[8 * (ks & 1) + 2 * i + 1], a.sl2, -ref));
+          part[ks] += e0;
+          part[ks] += e1;
+          pw[ks][i] = pack_bf16(e0, e1);
+        }
+      }
+      sum = (part[0] + part[1]) + (part[2] + part[3]);
+    };
+    probabilities();
+    if (__builtin_amdgcn_ballot_w64(!(sum <= kMostSum) || m == -INFINITY)) {
+      const float mx = max_of_halves(__builtin_fmaxf(max16(sc[0]), max16(sc[1]))) * a.sl2;
       const float mn = __builtin_fmaxf(m, mx);
       const float alpha = __builtin_amdgcn_exp2f(m - (mn == -INFINITY ? 0.0f : mn));
       m = mn;
+      ref = mn == -INFINITY ? 0.0f : mn;
       l *= alpha;
 #pragma unroll
       for (int i = 0; i < DT; ++i) o[i] *= alpha;
+      probabilities();
     }
-    const float ref = m == -INFINITY ? 0.0f : m;
+    l += sum;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      u32x4 pw;
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x16& x = sc[ks / 2];
-        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[8 * (ks & 1) + 2 * i], a.sl2, -ref));
-        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[8 * (ks & 1) + 2 * i + 1], a.sl2, -ref));
-        sum += e0 + e1;
-        pw[i] = pack_bf16(e0, e1);
-      }
-      l += sum;
-      p[ks] = __builtin_bit_cast(bf16x8, pw);
-    }
-    first_ops(j);
+    for (int ks = 0; ks < 4; ++ks) p[ks] = __builtin_bit_cast(bf16x8, pw[ks]);
+    static_for<kAhead>([&](auto n) EFQ_INLINE { read_op(slot, n); });
   };
 
   // The second group runs a phase behind the first.  bf16, step j: K tile
   // j + NB and V tile j + NB - 1 are asked for in M(j), into the places of tiles
   // j and j - 1, which both groups have read by then; before the barrier behind
   // M(j) a wave waits for its part of K tile j + 3 and V tile j + 2: the first
-  // group begins to read K tile j + 2 and V tile j + 1 in the phase after.  MXFP8 (NB = 3): K tile j + 3 and V tile j + 2 come into
-  // registers in M(j) and are written in V(j + 1).
+  // group begins to read K tile j + 2 and V tile j + 1 in the phase after.  (One
+  // group, NB = 3: for K tile j + 2 and V tile j + 1.)  MXFP8 (NB = 3): K tile
+  // j + 3 and V tile j + 2 come into registers in M(j) and are written in V(j + 1).
   constexpr int kLoads = 2 * Feed::PER;                     // of a wave in a step
   constexpr bool PAIR = NW == 8;
   constexpr int kKept = (PAIR ? NB - 3 : NB - 2) * kLoads;  // of them on their way at a wait
   if (ntiles > 0) {
-    ids = pages_from(0);
-    asked = pages_from(16);
-    bad = bad_of(ids);
-    fetch_k(0);
-    land_k(0);
-#pragma unroll
-    for (int t = 1; t < NB; ++t) {
-      fetch(t);
+    turn_page(0);
+    static_for<NB>([&](auto t) EFQ_INLINE {                 // (V of tile -1: no bytes)
+      fetch(t, decltype(t)::value);
       land(t);
-    }
+    });
     if constexpr (!F8) wait_vmem_le(kKept);
     wg_barrier();
-    if (mine > 0) scores(0);
-    phase_v(0);
+    if (mine > 0) {
+      static_for<NK>([&](auto n) EFQ_INLINE {
+        constexpr int N = NV + decltype(n)::value;
+        read_op(std::integral_constant<int, NB - 1>{}, std::integral_constant<int, N>{});
+        product(std::integral_constant<int, N>{});
+      });
+    }
+    phase_v(std::integral_constant<int, 0>{}, 0);
     wg_barrier();                                           // K tile 0 is read before its place is filled again
     const bool second = PAIR && wave >= NW / 2;
     if (second) wg_barrier();
-    for (int j = 0; j < ntiles; ++j) {
-      turn_page(j);
-      phase_m(j);
-      if constexpr (!F8) wait_vmem_le(kKept);
-      wg_barrier();
-      if (j + 1 < ntiles) phase_v(j + 1);
-      land(j + NB);
-      if constexpr (PAIR) wg_barrier();
-    }
+    for (int j0 = 0; j0 < ntiles; j0 += NB)
+      static_for<NB>([&](auto slot) EFQ_INLINE {
+        constexpr int SLOT = decltype(slot)::value;
+        const int j = j0 + SLOT;
+        if (j < ntiles) {
+          turn_page(j + NB);
+          phase_m(slot, j);
+          if constexpr (!F8) wait_vmem_le(kKept);
+          wg_barrier();
+          if (j + 1 < ntiles) phase_v(std::integral_constant<int, (SLOT + 1) % NB>{}, j + 1);
+          land(slot);
+          if constexpr (PAIR) wg_barrier();
+        }
+      });
     if (PAIR && !second) wg_barrier();
     if constexpr (!F8) wait_vmem();                         // nothing is on its way to LDS when it is given up
   }
