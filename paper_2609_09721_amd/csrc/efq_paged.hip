@@ -1361,8 +1361,8 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
   const long rows = most_q * G;
   // The chunk kernel's waves share what they read, the step kernel's rows all
   // pass through every wave.  32 rows: 16 sequences x 8 tokens over 4000 keys
-  // (32/8 heads, D 128, bf16) step 42 us, chunk 51; 64 rows: x 16 tokens 58 and
-  // 53, MXFP8 41 and 55; D 64, 4 sequences x 16 tokens 13.9 and 19.0.
+  // (32/8 heads, D 128, bf16) step 43 us, chunk 44; 64 rows: x 16 tokens 61 and
+  // 46, MXFP8 40 and 49; D 64, 4 sequences x 16 tokens 13.4 and 14.5.
   const bool low = c->format == EFQ_CACHE_MXFP8, narrow = c->head_dim == 64;
   p.rt = rows <= 16 ? 1 : rows <= (low || narrow ? 64 : 32) ? 2 : 0;
   p.bm = p.rt ? 16 * p.rt : narrow ? 128 : 256;
@@ -1371,27 +1371,27 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
   const long keys = std::min({(long)b->table_width * c->page_size, (long)kMostKeys, b->max_k ? (long)b->max_k : (long)kMostKeys});
   long n = 1;
   if (p.rt) {
-    // Splits of the longest sequence: as many as put two workgroups on every
-    // CU; sequences of different lengths (more than one) also want pieces small
-    // enough to end together, down to 448 KB of keys and values, which stream in
-    // about ten times what it takes to start a workgroup, while the unsplit call
-    // has fewer than eight rounds of workgroups.  17 sequences of 5000
-    // to 20000 keys (32/8 heads, D 128, bf16) in pieces of 6700 / 2900 / 1540 /
-    // 830 keys: 164 / 171 / 145 / 138 us; one of 131000 keys in 64 / 256 pieces
-    // 87 / 98 us.  Below 1024 keys the join costs more than it saves (one
-    // sequence of 500 keys in two 15.0 us, in one 10.9; of 2000 in 4 / 8 pieces
-    // 14.6 / 12.9).
+    // Splits of the longest sequence.  One sequence: as many as give every CU one
+    // workgroup (131000 keys, 32/8 heads, D 128, bf16, in 16 / 32 / 64 / 256 pieces
+    // 130 / 84 / 88 / 98 us; 8 tokens over 20000 in 16 / 32 / 64: 30 / 25 / 30).
+    // Several, whose lengths differ: two, and pieces small enough to end
+    // together, down to 448 KB of keys and values, which stream in about ten
+    // times what it takes to start a workgroup, while the unsplit call has fewer
+    // than eight rounds of workgroups (17 sequences of 5000 to 20000 keys in pieces
+    // of 6700 / 2900 / 1540 / 830 keys: 164 / 171 / 145 / 138 us).  Below 1024 keys
+    // the join costs more than it saves (one sequence of 500 keys in two 15.0 us,
+    // in one 10.9; of 2000 in 4 / 8 pieces 14.6 / 12.9).
     const long items = std::max<long>(1, p.slots * c->heads_kv);
     const long key_bytes = 2 * (low ? c->head_dim + c->head_dim / 32 : 2 * c->head_dim);
-    n = (2 * kCUs + items - 1) / items;
+    n = ((b->seqs > 1 ? 2 * kCUs : kCUs) + items - 1) / items;
     if (b->seqs > 1) n = std::max(n, std::min(keys * key_bytes / (448 << 10), 16 * kCUs / items));
     n = keys < 1024 ? 1 : std::max<long>(1, std::min(n, keys / 256));
   } else {
     // As many pieces (of at least 256 keys) as leave the chip one round of
     // workgroups, by the average of the sequences' rows; rounded up where lengths
-    // differ, since short sequences fill fewer.  64 tokens over 20000 keys (32/8 heads, D 128, bf16: 8
-    // workgroups unsplit) in 8 / 16 / 32 pieces 79 / 54 / 47 us, 700 tokens over
-    // 20000 (88) in 1 / 2 / 3 / 4 pieces 479 / 283 / 370 / 306.
+    // differ, since short sequences fill fewer.  64 tokens over 20000 keys (32/8
+    // heads, D 128, bf16: 8 workgroups unsplit) in 8 / 16 / 32 pieces 67 / 48 / 45
+    // us, 700 tokens over 20000 (88) in 1 / 2 / 3 / 4 pieces 394 / 251 / 329 / 275.
     const long items = b->seqs * (((long)b->tokens * G / b->seqs + p.bm - 1) / p.bm) * c->heads_kv;
     n = std::max<long>(1, std::min((kCUs + (b->seqs > 1 ? items / 2 : 0)) / std::max<long>(1, items), keys / 256));
   }
