@@ -336,8 +336,8 @@ typedef struct efq_rotary {
 } efq_rotary;
 
 /* y = x with its positions applied; inverse != 0 turns back, which is the
- * gradient: dx from dy.  y may be x (in place); other overlaps are not
- * supported.  head_dim a multiple of 16 up to 512, pairs a multiple of 8.
+ * gradient: dx from dy.  y may be x (in place, the strides alike); other
+ * overlaps are not supported.  head_dim a multiple of 16 up to 512, pairs a multiple of 8.
  * tokens == 0 does nothing. */
 int efq_rope(const efq_rows *x, const efq_rows *y, int tokens, int heads, int head_dim, int dtype,
              const efq_rotary *rot, int inverse, efq_stream_t stream);
@@ -363,7 +363,8 @@ typedef struct efq_cache {
  * they are not appended, and their outputs stay as they were.
  * tokens: rows of the call's tensors.  max_q, max_k: the largest number of new
  * tokens and of keys of a sequence as far as the host knows (0: unknown); they
- * choose how the work is split, and never change what is computed.
+ * choose how the work is split, so the order of sums, and wrong ones cost time,
+ * never a row's keys.
  * Values out of range do no harm: a page outside [0, pages) holds nothing
  * (nothing is written there, and its keys are not seen), lengths are cut to
  * the page table's width, starts to the call's tokens; a token before its
@@ -395,7 +396,10 @@ int efq_kv_append(const efq_rows *k, const efq_rows *v, const efq_cache *cache, 
  * and -inf.  Scores, sums and accumulators are fp32, the exponential is not
  * quantised; the probabilities enter the second product in bf16, relative
  * to the row's maximum.  What the cache holds outside the sequences (unused
- * slots and pages) may be anything; seen keys and values must be finite.
+ * slots and pages) may be anything; queries, and keys and values of the
+ * sequences, must be finite, scores within 2^30 (an fp32 score has no digit left
+ * for the exponential there) and values within 2^80 (sums are not normalised
+ * before the end).
  * Work is split over the keys where the rows alone do not fill the chip, which
  * takes scratch memory: ws of efq_attn_paged_workspace_bytes (0 where nothing
  * is split), 16-byte aligned; without it (NULL, 0) or with less, the call runs

@@ -381,11 +381,11 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // key/value head, row r = token r / G, head h G + r % G.  A workgroup takes
 // BM of them at a time.  In the step kernel, where the host knows of no sequence
 // with more than BM rows, slot n of the grid is sequence n, whose workgroup goes
-// on to further BM rows if there are any.  Otherwise slot n belongs to the last sequence i with
-// floor((q_start[i] - q_start[0]) G / BM) + i <= n, so that a sequence has at
-// least ceil(new G / BM) slots whatever the lengths, and the grid, which the
-// host knows without reading them, is ceil(tokens G / BM) + seqs - 1; slots
-// without rows leave at once.
+// on to further BM rows if there are any.  Otherwise slot n belongs to the last
+// sequence i with floor((q_start[i] - q_start[0]) G / BM) + i <= n, so that a
+// sequence has at least ceil(new G / BM) slots whatever the lengths, and the
+// grid, which the host knows without reading them, is ceil(tokens G / BM) +
+// seqs - 1; slots without rows leave at once.
 //
 // Both kernels compute scores transposed, S^T = K Q^T, so a lane owns one row
 // (column of the product), and O^T += V^T P^T with P^T taken from the score
@@ -462,18 +462,22 @@ __device__ __forceinline__ void put4(char* at, int f32, f32x4 o) {
 }
 
 // ---- one or a few tokens
-// Four waves of a workgroup take every fourth tile (16 kStepHalves keys) of a split's
-// keys, each with its own running maximum, sum and O^T, joined at the end
-// through LDS.  Nothing is shared while streaming, so there is no barrier in
-// the loop; a wave has one tile on its way while it works on the one before.
-// 16 RT rows: K in matrix-operand order straight into registers, V through LDS
-// for its transposition.
+// Four waves of a workgroup take every fourth tile (32 keys) of a split's keys,
+// each with its own running maximum, sum and O^T, joined at the end through LDS.
+// Nothing is shared while streaming, so there is no barrier in the loop; a wave
+// has one tile on its way while it works on the one before, 16 KB of bf16 at
+// D 128, 128 KB a CU with its two workgroups.  16 RT rows: K in matrix-operand
+// order straight into registers, V through LDS for its transposition.
+//
+// One token over 131000 keys (32/8 heads, D 128, bf16; 537 MB) takes 84 us, 6.35
+// TB/s, where a kernel that only reads reaches 6.0 to 6.2; 17 sequences of 5000
+// to 20000 keys (797 MB) 138 us, 5.8 TB/s.
 constexpr int kStepWaves = 4;
-constexpr int kStepHalves = 2;       // 16-key halves of a wave's tile
+constexpr int kStepHalves = 2;     // 16-key halves of a wave's tile
 
 template <int D, int RT>
 struct StepLds {
-  static constexpr int kV = 16 * kStepHalves * D * 2;                         // V tile of a wave
+  static constexpr int kV = 16 * kStepHalves * D * 2;                // V tile of a wave
   static constexpr int kO = 16 * RT * (D + 4) * 4;                   // O of a wave
   static constexpr int kWave = kV > kO ? kV : kO;
   static constexpr int kTotal = kStepWaves * (kWave + 16 * RT * 8);  // and maximum, sum
@@ -497,7 +501,7 @@ struct StepTile {
   static constexpr int VN = kStepHalves * (F8 ? D / 64 : D / 32);  // 16-byte pieces of V a lane
   static constexpr int VROWS = F8 ? 1024 / D : 512 / D;   // V rows of one load
   u32x4 k[kStepHalves][KN], v[VN];
-  unsigned ksc[F8 ? kStepHalves : 1], vsc[F8 ? VN : 1];            // a K row's scales, a V piece's scale
+  unsigned ksc[F8 ? kStepHalves : 1], vsc[F8 ? VN : 1];   // a K row's scales, a V piece's scale
   __device__ __forceinline__ void load_k(const PagedArgs& a, const long* row, int lane) {
     const unsigned r = lane & 15, g = lane >> 4;
 #pragma unroll
@@ -574,9 +578,9 @@ __device__ __forceinline__ void step_rows(const PagedArgs& a, Slot& s, int h, in
   const int wave = uniform(threadIdx.x >> 6);
   const int g = lane >> 4, col = lane & 15;
 
-  // The wave's tiles begin at k0 + KEYS wave + ROUND it; lane kStepHalves (it % AHEAD) +
-  // half holds the page of that tile's half, for AHEAD tiles at a time.  The
-  // first ones, and Q, are asked for beside the sequence's length.
+  // The wave's tiles begin at k0 + KEYS wave + ROUND it; lane kStepHalves (it %
+  // AHEAD) + half holds the page of that tile's half, for AHEAD tiles at a time.
+  // The first ones, and Q, are asked for beside the sequence's length.
   const int k0 = (int)min((long)sp * a.chunk, (long)kMostKeys);
   const int32_t* table = a.b.table + (long)s.seq * a.b.width;
   auto pages_from = [&](int it) {
@@ -773,13 +777,22 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
 }
 
 // ---- many tokens
-// Waves of 32 rows share 64-key tiles of K and V in LDS, two of each.  A SIMD
-// overlaps its matrix core and its vector unit when one of its two waves does
-// only matrix work and the other only vector work, not when both do some of
-// each; so the waves form two groups that swap phases at a barrier: while one
-// group runs M (scores of tile j + 1, P V of tile j: 32 matrix instructions at
-// D 128), the other runs V (maxima and exponentials of a tile).  K runs one
-// tile ahead of V, the loads one tile ahead of both.
+// Waves of 32 rows share 64-key tiles of K and V in LDS, in rings of three or
+// four.  A SIMD overlaps its matrix core and its vector unit when one of its two
+// waves does only matrix work and the other only vector work, not when both do
+// some of each; so at D 128 eight waves form two groups that swap phases at a
+// barrier: while one group runs M (P V of tile j, scores of tile j + 1: 32 matrix
+// instructions), the other runs V (exponentials of a tile).  At D 64 a phase is
+// too short for that (a barrier costs a tenth of it) and rows are short enough
+// for three workgroups of four waves a CU, which overlap by themselves.
+//
+// 2048 tokens behind 14000 keys (32/8 heads, D 128, bf16; 504 GFLOP) take 418
+// us, 1206 TFLOP/s; 4096 behind 28000, MXFP8, 1620 us, 1244.  The matrix core is
+// busy 63 % of the cycles and the chip lowers its clock to 1.77 GHz for the power
+// (on keys and values of one constant it runs at 2.23).  D 64, 7 sequences of
+// 1500 tokens (12/12 heads): 79 us, 726 TFLOP/s; its 16 exponentials and 8
+// matrix instructions a lane and tile half take 256 cycles each, and the vector
+// unit has sums, scaling and packing besides.
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
   if constexpr (I < N) {
@@ -804,10 +817,10 @@ __device__ __forceinline__ int chunk_v_swz(int r) { return D == 128 ? ((r & 3) <
 
 // One 1 KB direct-to-LDS load through a buffer resource (address, bytes): lane
 // i's 16 bytes at voff land at LDS address `to` + 16 i, zeros where voff is past
-// the resource's bytes.  In assembly, since
-// the compiler would wait for all such loads before the next transposing read;
-// it has no register output, and the kernel's own waits count it.  Waits that
-// the compiler places for its loads count it too, and so only wait longer.
+// the resource's bytes.  In assembly, since the compiler would wait for all such
+// loads before the next transposing read; it has no register output, and the
+// kernel's own waits count it.  Waits that the compiler places for its loads
+// count it too, and so only wait longer.
 __device__ __forceinline__ void load_lds_1k(u32x4 rsrc, unsigned to, int voff) {
   // (five wait states from a vector instruction that writes a scalar register to
   // a memory instruction that reads it, one from the write of m0, which the
@@ -829,7 +842,7 @@ __device__ __forceinline__ unsigned raw_load1(const char* from, unsigned bytes, 
 // What brings the K and V tiles of one slot into LDS.  A wave brings the same 8
 // or 16 rows of every tile, which lie in one page.  Where they lie is worked out
 // for 64 tiles at once, lane t for tile t of a group, so that a step only reads
-// it out of the lane; the pages of the next group are asked for meanwhile.
+// it out of the lane.
 template <int D, bool F8, int NW>
 struct ChunkFeed {
   static constexpr int RB = F8 ? D : 2 * D;                 // bytes of a row
@@ -925,7 +938,7 @@ struct ChunkFeed {
 // lane's probabilities of a tile sum up to more than this, so almost never
 // after the first tile, and until then no maximum is taken and nothing rescaled.
 // It costs no precision (the probabilities' rounding is relative, the sums are
-// fp32 and stay far below their range).
+// fp32: 2^16 a tile and lane, so below 2^42 in all, times the values).
 constexpr float kMostSum = 65536.0f;
 
 // One slot's rows, split sp of their keys.
@@ -1278,14 +1291,18 @@ int check_rows(const efq_rows* r, const char* name, int es) {
     return fail(EFQ_EINVAL, "%s: strides must be multiples of 16 bytes", name);
   return EFQ_OK;
 }
-// Rows that are written: no two heads or tokens may lie on each other.
-int check_out_rows(const efq_rows* r, const char* name, int es, int tokens, int heads, int head_dim) {
+// Rows that are written: no two heads or tokens may lie on each other, and where
+// they begin with those of `in` they are those, row for row.
+int check_out_rows(const efq_rows* r, const char* name, int es, int tokens, int heads, int head_dim,
+                   const efq_rows* in = nullptr) {
   const int rc = check_rows(r, name, es);
   if (rc) return rc;
   if ((heads > 1 && r->head < head_dim) || (tokens > 1 && r->token < head_dim) ||
       (heads > 1 && tokens > 1 && r->token < r->head * (heads - 1) + head_dim &&
        r->head < r->token * (tokens - 1) + head_dim))
     return fail(EFQ_EINVAL, "%s: rows overlap", name);
+  if (in && in->data == r->data && ((tokens > 1 && in->token != r->token) || (heads > 1 && in->head != r->head)))
+    return fail(EFQ_EINVAL, "%s: in place, but with other strides", name);
   return EFQ_OK;
 }
 
@@ -1395,7 +1412,6 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
     const long items = b->seqs * (((long)b->tokens * G / b->seqs + p.bm - 1) / p.bm) * c->heads_kv;
     n = std::max<long>(1, std::min((kCUs + (b->seqs > 1 ? items / 2 : 0)) / std::max<long>(1, items), keys / 256));
   }
-  n = std::min<long>(n, 4096);             // within a grid's second dimension
   p.chunk = (int)(((keys + n - 1) / n + 127) / 128 * 128);
   p.nsplit = (int)std::max<long>(1, (keys + p.chunk - 1) / p.chunk);
   p.bytes = p.nsplit == 1 ? 0 : round256((size_t)p.nsplit * b->tokens * heads_q * 8) +
@@ -1470,7 +1486,7 @@ int efq_rope(const efq_rows* x, const efq_rows* y, int tokens, int heads, int he
   const int es = dtype == EFQ_F32 ? 4 : 2;
   int rc;
   if ((rc = check_rotary(rot, head_dim)) || (rc = check_rows(x, "x", es)) ||
-      (rc = check_out_rows(y, "y", es, tokens, heads, head_dim)))
+      (rc = check_out_rows(y, "y", es, tokens, heads, head_dim, x)))
     return rc;
   if ((rc = check_device())) return rc;
   RopeArgs a;
@@ -1507,7 +1523,7 @@ int efq_kv_append(const efq_rows* k, const efq_rows* v, const efq_cache* cache, 
   if (batch->tokens == 0) return EFQ_OK;
   if ((rc = check_rows(k, "k", 2)) || (rc = check_rows(v, "v", 2))) return rc;
   if (rot && (rc = check_rotary(rot, D))) return rc;
-  if (q && ((rc = check_rows(q, "q", 2)) || (rc = check_out_rows(q_out, "q_out", 2, batch->tokens, heads_q, D)))) return rc;
+  if (q && ((rc = check_rows(q, "q", 2)) || (rc = check_out_rows(q_out, "q_out", 2, batch->tokens, heads_q, D, q)))) return rc;
   if ((rc = check_device())) return rc;
   AppendArgs a;
   memset(&a, 0, sizeof a);

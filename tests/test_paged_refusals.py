@@ -52,8 +52,9 @@ def refused(L, rc, status):
     (dict(y=dict(token=512, head=128)), -1), (dict(y=dict(token=128, head=256)), -1),
     (dict(rot=dict(pairs=0)), -1), (dict(rot=dict(pairs=72)), -1), (dict(rot=dict(pairs=60)), -2), (dict(rot=dict(axes=0)), -1),
     (dict(rot=dict(inv=None)), -1), (dict(rot=dict(pos=None)), -1), (dict(rot=None), -1), (dict(), VALID),
-    (dict(x=dict(token=0, head=0)), VALID),                       # a broadcast input
-    (dict(y=dict(token=128, head=128 * 5)), VALID),               # heads outermost
+    (dict(x=dict(token=0, head=0, data=FAKE + 65536)), VALID),    # a broadcast input
+    (dict(x=dict(token=0, head=0)), -1), (dict(x=dict(token=2048)), -1), (dict(x=dict(token=2048), tokens=1), VALID),  # in place
+    (dict(y=dict(token=128, head=128 * 5, data=FAKE + 65536)), VALID),      # heads outermost
     (dict(tokens=0, x=dict(data=None), y=dict(data=None)), 0)])
 def test_rope(L, kw, status):
     if status == VALID:
@@ -103,6 +104,7 @@ def test_append_arguments(L):
     refused(L, f(hq=4), -1)                                          # heads without q
     refused(L, f(q=r, hq=32), -1)                                    # no q_out
     refused(L, f(q=r, hq=32, o=rows(L, token=2048)), -1)             # its rows overlap
+    refused(L, f(q=r, hq=32, o=rows(L, token=8192)), -1)             # in place, but other strides
     refused(L, lib.efq_kv_append(r, r, None, b, None, None, 0, None, None), -1)
     refused(L, lib.efq_kv_append(r, r, c, None, None, None, 0, None, None), -1)
     assert f(k=None, v=None, bb=batch(L, tokens=0)) == 0
