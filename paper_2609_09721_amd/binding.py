@@ -523,6 +523,8 @@ def rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, axis: Optio
         out = torch.empty(x.shape, dtype=dtype, device=x.device)
     elif out.shape != x.shape:
         raise ValueError("out must have the shape of x")
+    if not x.is_cuda:
+        raise ValueError("x must be a CUDA tensor")
     dev = torch.cuda.current_device()
     xs = _tokens(x)
     xr, yr = _rows(xs, "x", dtype, dev), _rows(_tokens(out), "out", dtype, dev)
