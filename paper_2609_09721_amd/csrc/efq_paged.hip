@@ -1395,14 +1395,16 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
     // together, down to 448 KB of keys and values, which stream in about ten
     // times what it takes to start a workgroup, while the unsplit call has fewer
     // than eight rounds of workgroups (17 sequences of 5000 to 20000 keys in pieces
-    // of 6700 / 2900 / 1540 / 830 keys: 164 / 171 / 145 / 138 us).  Below 1024 keys
-    // the join costs more than it saves (one sequence of 500 keys in two 15.0 us,
-    // in one 10.9; of 2000 in 4 / 8 pieces 14.6 / 12.9).
+    // of 6700 / 2900 / 1540 / 830 keys: 164 / 171 / 145 / 138 us).  The join costs
+    // a launch, so short sequences stay whole (one of 500 keys in one piece 8.3 us,
+    // in two 12.9; 8 of 600 12.0 and 12.9, of 800 15.6 and in four 12.8; 8 tokens
+    // over 600 keys 13.2 and 13.0, over 800 15.6 and 13.1; D 64, 1000 keys 8.2 and
+    // 12.0), and pieces have 192 keys at least.
     const long items = std::max<long>(1, p.slots * c->heads_kv);
     const long key_bytes = 2 * (low ? c->head_dim + c->head_dim / 32 : 2 * c->head_dim);
     n = ((b->seqs > 1 ? 2 * kCUs : kCUs) + items - 1) / items;
     if (b->seqs > 1) n = std::max(n, std::min(keys * key_bytes / (448 << 10), 16 * kCUs / items));
-    n = keys < 1024 ? 1 : std::max<long>(1, std::min(n, keys / 256));
+    n = keys < (narrow ? 1024 : p.rt == 2 ? 640 : 768) ? 1 : std::max<long>(1, std::min(n, keys / 192));
   } else {
     // As many pieces (of at least 256 keys) as leave the chip one round of
     // workgroups, by the average of the sequences' rows; rounded up where lengths
