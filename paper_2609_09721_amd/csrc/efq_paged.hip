@@ -18,6 +18,7 @@
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
@@ -105,6 +106,16 @@ struct RopeArgs {
 // (32/8 heads, D 128, bf16) 99.9 -> 87.5 us (5.37 -> 6.13 TB/s), 300 tokens over
 // 1000 keys each 141 -> 131 us.
 __device__ __forceinline__ u32x4 stream16(const char* p) { return __builtin_nontemporal_load((const u32x4*)p); }
+// So do writes that the last-level cache (256 MB) would not hold until they are
+// read, or whose reader works long on each: 32760 tokens of 24 heads of 128 turned in
+// fp32 (403 MB) 139 -> 131 us, but 60000 of 8 (246 MB) 73 -> 81; 16000 tokens
+// (32/8 heads, D 128) appended to bf16 pages 87 -> 79, 11400 to MXFP8 ones 62 -> 58.
+constexpr long kLastLevel = 256 << 20;
+template <bool STREAM, typename T>         // (at compile time: a branch would be merged into one plain store)
+__device__ __forceinline__ void put(char* p, T x) {
+  if constexpr (STREAM) __builtin_nontemporal_store(x, (T*)p);
+  else *(T*)p = x;
+}
 
 // The values of 16-byte pieces.
 template <bool F32>
@@ -142,15 +153,14 @@ __device__ __forceinline__ void turn_halves(Piece<F32>& lo, Piece<F32>& hi, cons
   }
 }
 
-constexpr int kRopeTokens = 8;     // most tokens of a workgroup
-constexpr int kRopePairs = 256;    // most pairs of a head
+constexpr int kMostShared = 4;     // most tokens of a workgroup
 
 // An item is a 16-byte piece of a head (neighbouring pairs) or the two pieces of
 // the same pairs (halves), so that the lanes of a load lie side by side; pieces
 // behind the pairs pass through.  Every value is read once, past the caches.  A
 // thread has several items on their way at once, found by stepping (token, head,
 // chunk) on, since a division an item would cost as much as the turn.
-template <bool F32, bool INTERLEAVED>
+template <bool F32, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
   extern __shared__ float2 rot[];          // [tt][pairs]
   const long t0 = (long)blockIdx.x * a.tt;
@@ -192,9 +202,9 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
           if (vc[u] < turned) turn_beside(lo[u], cs);
         } else {
           if (vc[u] < turned) turn_halves(lo[u], hi[u], cs);
-          *(u32x4*)(y + at_hi(u)) = hi[u].w;
+          put<STREAM>(y + at_hi(u), hi[u].w);
         }
-        *(u32x4*)(y + at_lo(u)) = lo[u].w;
+        put<STREAM>(y + at_lo(u), lo[u].w);
       }
   }
 }
@@ -276,16 +286,18 @@ __device__ __forceinline__ u32x4 turn8(u32x4 w, u32x4 o, int c, const RotArgs& r
 // 32-value block of MXFP8 is four neighbouring lanes, as in mxfp8_block, and the
 // other halves of a turned row's pairs are in its lanes.  A workgroup's tokens
 // are walked through head by head, since a page holds a head's tokens side by
-// side: 13000 tokens (32/8 heads, D 128) into MXFP8 pages 78 -> 60 us.
+// side: 11400 tokens (32/8 heads, D 128) into MXFP8 pages 78 -> 60 us.
 // In place (q_out = q) a row's loads precede its stores: the row belongs to one
 // instruction of one wave.
 // With several tokens to a workgroup (MANY) a thread has four rows on their way
-// at once and loads past the caches; few tokens, whose rows were written just
-// before, are taken from them: 2000 tokens into bf16 pages 12.8 us, 17.6 as many.
+// at once and loads and stores past the caches; few tokens, whose rows were written
+// just before, are taken from them: 2000 tokens into bf16 pages 12.8 us, 17.6 as
+// many.  16000 tokens (393 MB) 79 us, 5.0 TB/s, 11400 into MXFP8 pages (258 MB) 58
+// us, 4.4: the writes are scattered, a head's tokens at a time.
 template <int D, bool F8, bool MANY>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
   extern __shared__ float2 rot[];          // [tt][pairs]
-  __shared__ long slot[kRopeTokens];       // row of head 0 in the cache, -1: none
+  __shared__ long slot[kMostShared];       // row of head 0 in the cache, -1: none
   constexpr int C = D / 8, U = MANY ? 4 : 1;
   const long t0 = (long)blockIdx.x * a.tt;
   const int nt = (int)min((long)a.tt, a.b.tokens - t0);
@@ -346,12 +358,12 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
         if (turned) x = turn8(x, o, c, a.rot, rot + vt[u] * pairs);
       }
       if (is_q) {
-        *(u32x4*)(a.qo + (t0 + vt[u]) * a.o_token + (vr[u] - 2 * a.heads) * a.o_head + 16 * c) = x;
+        put<MANY>(a.qo + (t0 + vt[u]) * a.o_token + (vr[u] - 2 * a.heads) * a.o_head + 16 * c, x);
         continue;
       }
       const long to = s + ((long)(is_v ? vr[u] - a.heads : vr[u]) << a.b.shift);
       if constexpr (!F8) {
-        *(u32x4*)((is_v ? a.vc : a.kc) + to * (2 * D) + 16 * c) = x;
+        put<MANY>((is_v ? a.vc : a.kc) + to * (2 * D) + 16 * c, x);
       } else {
         unsigned am = 0;
 #pragma unroll
@@ -369,7 +381,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
           z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y(bf16_lo(x[2 * j + 1])), y(bf16_hi(x[2 * j + 1])), 1.0f, true);
           p[j] = __builtin_bit_cast(unsigned, z);
         }
-        *(uint2*)((is_v ? a.vc : a.kc) + to * D + 8 * c) = make_uint2(p[0], p[1]);
+        put<MANY>((is_v ? a.vc : a.kc) + to * D + 8 * c, u32x2{p[0], p[1]});
         if ((c & 3) == 0) (is_v ? a.vs : a.ks)[to * (D / 32) + c / 4] = (uint8_t)(k + 127);
       }
     }
@@ -789,8 +801,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
 // 2048 tokens behind 14000 keys (32/8 heads, D 128, bf16; 504 GFLOP) take 418
 // us, 1206 TFLOP/s; 4096 behind 28000, MXFP8, 1620 us, 1244.  The matrix core is
 // busy 63 % of the cycles and the chip lowers its clock to 1.77 GHz for the power
-// (on keys and values of one constant it runs at 2.23).  D 64, 7 sequences of
-// 1500 tokens (12/12 heads): 79 us, 726 TFLOP/s; its 16 exponentials and 8
+// (on keys and values of one constant it runs at 2.23).  D 64, 7 sequences of up to
+// 1500 tokens behind 3001 (16/4 heads): 80 us, 718 TFLOP/s; its 16 exponentials and 8
 // matrix instructions a lane and tile half take 256 cycles each, and the vector
 // unit has sums, scaling and packing besides.
 template <int N, int I = 0, typename F>
@@ -1350,12 +1362,24 @@ Batch batch_args(const efq_batch* b, const efq_cache* c) {
 
 // Tokens of a workgroup (a power of two) and workgroups of a token in the kernels
 // that walk over tokens: few tokens are spread over the chip a workgroup per 256
-// threads' work, many share one workgroup as long as eight are left for a CU.
-void token_grid(int tokens, int threads_per_token, int& tt, int& parts) {
-  for (tt = kRopeTokens; tt > 1 && tokens < tt * 8 * kCUs; tt /= 2) {}
+// threads' work, many share one workgroup as long as eight are left for a CU, and
+// no more than `enough` work needs: short workgroups keep a CU's reads and writes
+// mixed.  rope, enough 768 pieces of 16 bytes (an item of halves is two): 32760
+// tokens of 768 pieces (fp32) at 1 / 2 / 4 / 8 tokens 139 / 149 / 156 / 163 us, 8192 of 640 (bf16)
+// 30.7 / 30.6 / 32.2, 20000 of 128 23.8 / 19.2 / 16.8 / 18.0.  Append, whose pages hold
+// a head's tokens side by side: 11400 tokens (32/8 heads, D 128) into MXFP8 pages at
+// 1 / 2 / 4 / 8 tokens 71 / 64 / 61 / 65 us.
+void token_grid(int tokens, int threads_per_token, int enough, int& tt, int& parts) {
+  for (tt = kMostShared; tt > 1 && (tokens < tt * 8 * kCUs || tt / 2 * threads_per_token >= enough); tt /= 2) {}
   parts = tt > 1 || tokens > 4 * kCUs ? 1 : (threads_per_token + 255) / 256;
 }
 
+template <bool F32, bool INTERLEAVED>
+hipError_t launch_rope(const RopeArgs& a, dim3 grid, int lds, bool stream_out, hipStream_t st) {
+  if (stream_out) hipLaunchKernelGGL((rope_kernel<F32, INTERLEAVED, true>), grid, dim3(256), lds, st, a);
+  else hipLaunchKernelGGL((rope_kernel<F32, INTERLEAVED, false>), grid, dim3(256), lds, st, a);
+  return hipGetLastError();
+}
 template <int D, bool F8, bool MANY>
 hipError_t launch_append(const AppendArgs& a, dim3 grid, int lds, hipStream_t st) {
   hipLaunchKernelGGL((kv_append_kernel<D, F8, MANY>), grid, dim3(256), lds, st, a);
@@ -1498,17 +1522,16 @@ int efq_rope(const efq_rows* x, const efq_rows* y, int tokens, int heads, int he
   a.tokens = tokens, a.heads = heads, a.chunks = head_dim * es / (rot->interleaved ? 16 : 32), a.inverse = inverse != 0;
   a.rot = rot_args(rot, tokens);
   int parts;
-  token_grid(tokens, heads * a.chunks, a.tt, parts);
+  token_grid(tokens, heads * a.chunks, rot->interleaved ? 768 : 384, a.tt, parts);
   const int step = 256 * parts, per = heads * a.chunks;
   a.dt = step / per, a.dh = step % per / a.chunks, a.dc = step % a.chunks;
   const dim3 grid((unsigned)(((long)tokens + a.tt - 1) / a.tt), (unsigned)parts);
   const int lds = a.tt * rot->pairs * (int)sizeof(float2);
   hipStream_t st = (hipStream_t)stream;
-  if (es == 4 && rot->interleaved) hipLaunchKernelGGL((rope_kernel<true, true>), grid, dim3(256), lds, st, a);
-  else if (es == 4) hipLaunchKernelGGL((rope_kernel<true, false>), grid, dim3(256), lds, st, a);
-  else if (rot->interleaved) hipLaunchKernelGGL((rope_kernel<false, true>), grid, dim3(256), lds, st, a);
-  else hipLaunchKernelGGL((rope_kernel<false, false>), grid, dim3(256), lds, st, a);
-  hipError_t e = hipGetLastError();
+  const bool stream_out = (long)tokens * heads * head_dim * es > kLastLevel;
+  hipError_t e;
+  if (es == 4) e = rot->interleaved ? launch_rope<true, true>(a, grid, lds, stream_out, st) : launch_rope<true, false>(a, grid, lds, stream_out, st);
+  else e = rot->interleaved ? launch_rope<false, true>(a, grid, lds, stream_out, st) : launch_rope<false, false>(a, grid, lds, stream_out, st);
   if (e != hipSuccess) return fail(EFQ_EHIP, "rope launch: %s", hipGetErrorString(e));
   return EFQ_OK;
 }
@@ -1542,7 +1565,7 @@ int efq_kv_append(const efq_rows* k, const efq_rows* v, const efq_cache* cache, 
   if (rot) a.rotate = 1, a.rot = rot_args(rot, batch->tokens);
   int parts;
   const int rows = 2 * a.heads + heads_q;
-  token_grid(batch->tokens, rows * (D / 8), a.tt, parts);
+  token_grid(batch->tokens, rows * (D / 8), 1 << 30, a.tt, parts);
   a.log_tt = __builtin_ctz((unsigned)a.tt);
   const dim3 grid((unsigned)(((long)batch->tokens + a.tt - 1) / a.tt), (unsigned)parts);
   const int lds = rot ? a.tt * rot->pairs * (int)sizeof(float2) : 0;

@@ -235,3 +235,17 @@ def test_append_lengths_out_of_range(B):
     assert go([0, 2], [1000], [[1]]) == {(1, 14): 0, (1, 15): 1}       # cut to the table's 16 keys
     assert go([0, 2], [-5], [[1]]) == {}
     assert go([-4, 4, 2, 900], [4, 1, 16], [[0], [1], [1]]) .keys() <= {(p, o) for p in range(2) for o in range(16)}
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype,tokens", [(torch.bfloat16, 33000), (torch.float32, 17000)])
+def test_rope_past_the_last_cache(B, dtype, tokens, interleaved):
+    """An output of more than 256 MB, whose writes are streamed, is that of its parts, which are not."""
+    x = torch.randn(tokens, 32, 128, device="cuda").to(dtype)
+    pos = torch.randint(0, 100000, (tokens,), dtype=torch.int32, device="cuda")
+    inv = (10000.0 ** (-torch.arange(64) / 64)).float().cuda()
+    assert x.numel() * x.element_size() > 256 << 20
+    whole = B.rope(x, pos, inv, interleaved=interleaved)
+    for t in range(0, tokens, 7001):
+        part = slice(t, t + 7001)
+        assert torch.equal(whole[part], B.rope(x[part], pos[part].contiguous(), inv, interleaved=interleaved))
