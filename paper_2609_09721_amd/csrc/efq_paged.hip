@@ -1414,12 +1414,16 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
   const long keys = std::min({(long)b->table_width * c->page_size, (long)kMostKeys, b->max_k ? (long)b->max_k : (long)kMostKeys});
   long n = 1;
   if (p.rt) {
-    // Splits of the longest sequence.  One sequence: as many as give every CU one
-    // workgroup (131000 keys, 32/8 heads, D 128, bf16, in 16 / 32 / 64 / 256 pieces
-    // 130 / 84 / 88 / 98 us; 8 tokens over 20000 in 16 / 32 / 64: 30 / 25 / 30).
-    // Several, whose lengths differ: two, and pieces small enough to end
-    // together, down to 448 KB of keys and values, which stream in about ten
-    // times what it takes to start a workgroup, while the unsplit call has fewer
+    // Splits of the longest sequence.  A CU reads no faster with two workgroups than
+    // with one, and the whole chip's as fast as HBM gives, so what counts is that
+    // each CU has as much as every other.  One workgroup for (nearly) every CU, where
+    // the items come out so: one sequence of 131000 keys (32/8 heads, D 128, bf16) in
+    // 16 / 32 / 64 / 256 pieces 130 / 84 / 88 / 98 us, 8 of 16000 in 2 / 4 / 8 / 16
+    // 108 / 66 / 69 / 70, 3 of 30000 in 8 / 10 / 16 59 / 52 / 62, 8 x 5 tokens over 6000
+    // in 2 / 4 / 8 47 / 32 / 36.  Single tokens over MXFP8 pages want two, one converts
+    // while the other waits: 8 of 16000 in 4 / 8 / 16 47 / 43 / 44.  Else two, and pieces small
+    // enough to end together, down to 448 KB of keys and values, which stream in about
+    // ten times what it takes to start a workgroup, while the unsplit call has fewer
     // than eight rounds of workgroups (17 sequences of 5000 to 20000 keys in pieces
     // of 6700 / 2900 / 1540 / 830 keys: 164 / 171 / 145 / 138 us).  The join costs
     // a launch, so short sequences stay whole (one of 500 keys in one piece 8.3 us,
@@ -1428,8 +1432,14 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
     // 12.0), and pieces have 192 keys at least.
     const long items = std::max<long>(1, p.slots * c->heads_kv);
     const long key_bytes = 2 * (low ? c->head_dim + c->head_dim / 32 : 2 * c->head_dim);
-    n = ((b->seqs > 1 ? 2 * kCUs : kCUs) + items - 1) / items;
-    if (b->seqs > 1) n = std::max(n, std::min(keys * key_bytes / (448 << 10), 16 * kCUs / items));
+    const long even = kCUs / items, idle = kCUs - even * items;
+    if (b->seqs == 1) {
+      n = (kCUs + items - 1) / items;
+    } else if (!(low && p.rt == 1) && even >= 2 && idle <= (even >= 4 ? kCUs / 8 : 0)) {
+      n = even;
+    } else {
+      n = std::max((2 * kCUs + items - 1) / items, std::min(keys * key_bytes / (448 << 10), 16 * kCUs / items));
+    }
     n = keys < (narrow ? 1024 : p.rt == 2 ? 640 : 768) ? 1 : std::max<long>(1, std::min(n, keys / 192));
   } else {
     // As many pieces (of at least 256 keys) as leave the chip one round of
