@@ -268,3 +268,11 @@ def test_offsets_past_32_bits(B, fmt):
     for i, p in enumerate(far):
         n = min(page, 600 - i * page)                # the slots behind them were never written
         assert torch.equal(cache.k[p, :, :n], small.k[i, :, :n]) and torch.equal(cache.v[p, :, :n], small.v[i, :, :n])
+
+
+@pytest.mark.parametrize("heads,D", [((7, 1), 64), ((33, 3), 128), ((100, 4), 64), ((48, 1), 128), ((130, 2), 128), ((5, 5), 64)])
+@pytest.mark.parametrize("new,keys", [([1, 1, 1], [90, 700, 1]), ([5, 1, 9], [300, 64, 9]), ([70, 33], [500, 40])])
+def test_any_number_of_heads_to_a_key(B, heads, D, new, keys):
+    c = Case(B, new, keys, heads, D, 32, "bf16", seed=30, pad=1)
+    out, lse, scale = run(B, c)
+    check(c, out, lse, scale, True)
