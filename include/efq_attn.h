@@ -366,9 +366,12 @@ typedef struct efq_cache {
  * choose how the work is split, so the order of sums, and wrong ones cost time,
  * never a row's keys.
  * Values out of range do no harm: a page outside [0, pages) holds nothing
- * (nothing is written there, and its keys are not seen), lengths are cut to
- * the page table's width, starts to the call's tokens; a token before its
- * sequence's first key (more new tokens than keys) is not appended. */
+ * (nothing is written there, and its keys are not seen).  Token j of a sequence
+ * is its key seq_k[i] - q_start[i + 1] + j whatever these are: one before the
+ * first key (more new tokens than keys) or past the page table (or past 2^30
+ * keys) is not appended, so no older key is written over, and sees the keys up
+ * to its own that the table holds.  Tokens outside the call's are none.  (To
+ * attention a length past 2^30 is the table's.) */
 typedef struct efq_batch {
     int seqs, tokens, table_width, max_q, max_k;
     const int32_t *q_start;     /* [seqs + 1], rising from 0                  */

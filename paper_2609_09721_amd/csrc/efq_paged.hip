@@ -218,9 +218,12 @@ struct Batch {
   const int32_t *q_start, *seq_k, *table;
   int seqs, tokens, width, pages, shift;   // page_size = 1 << shift
   __device__ __forceinline__ int start(int i) const { return min(max(q_start[i], 0), tokens); }
-  __device__ __forceinline__ int keys(int i) const {
-    return (int)min((long)max(seq_k[i], 0), min((long)width << shift, (long)kMostKeys));
-  }
+  __device__ __forceinline__ long room() const { return min((long)width << shift, (long)kMostKeys); }
+  // keys of sequence i that its table has slots for
+  __device__ __forceinline__ int keys(int i) const { return (int)min((long)max(seq_k[i], 0), room()); }
+  // Key of token t of sequence i, from its length and its end as they are given: one
+  // that was cut would put a token that the table has no slot for on an older key's.
+  __device__ __forceinline__ long key_of(int i, int t) const { return (long)seq_k[i] - q_start[i + 1] + t; }
 };
 
 // The last sequence i with at(i, start(i)) <= x, -1 for none, where at rises;
@@ -311,8 +314,8 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     long s = -2;                           // padding: nothing of the token is written
     if (i >= 0 && tok < end) {
       s = -1;
-      const long at = (long)a.b.keys(i) - end + tok;
-      if (at >= 0) {
+      const long at = a.b.key_of(i, tok);
+      if (at >= 0 && at < a.b.room()) {
         const int page = a.b.table[(long)i * a.b.width + (at >> a.b.shift)];
         if ((unsigned)page < (unsigned)a.b.pages)
           s = (((long)page * a.heads) << a.b.shift) + (at & ((1 << a.b.shift) - 1));
@@ -429,9 +432,10 @@ struct PagedArgs {
 
 struct Slot {
   int seq, row0, rows, q0, new_, keys;     // first row, rows of the slot; first token, new tokens, keys
+  int key0;                                // key of the first token
 };
 
-// The slot but for `keys`, which the caller loads beside what else it knows to
+// The slot but for its keys, which the caller loads beside what else it knows to
 // ask for by then.
 template <int BM>
 __device__ __forceinline__ bool find_slot(const PagedArgs& a, int n, Slot& s) {
@@ -460,9 +464,17 @@ __device__ __forceinline__ bool next_rows(const PagedArgs& a, Slot& s) {
   return a.direct && s.rows > 0;
 }
 
+// The slot's keys.  (Tokens past the table see what it holds.  A length that no
+// sequence has, past kMostKeys, is the table's.)
+__device__ __forceinline__ void find_keys(const PagedArgs& a, Slot& s) {
+  s.keys = a.b.keys(s.seq);
+  long at = a.b.key_of(s.seq, s.q0);
+  if (a.b.seq_k[s.seq] > kMostKeys) at = (long)s.keys - s.new_;
+  s.key0 = (int)min(max(at, -(long)kMostKeys), (long)kMostKeys);
+}
 // Keys that row r of the slot sees.
 __device__ __forceinline__ int seen(const PagedArgs& a, const Slot& s, int r) {
-  return a.causal ? max(s.keys - s.new_ + (s.row0 + r) / a.G + 1, 0) : s.keys;
+  return a.causal ? min(max(s.key0 + (s.row0 + r) / a.G + 1, 0), s.keys) : s.keys;
 }
 
 __device__ __forceinline__ int splits_of(const PagedArgs& a, int keys) {
@@ -611,10 +623,10 @@ __device__ __forceinline__ void step_rows(const PagedArgs& a, Slot& s, int h, in
 #pragma unroll
     for (int i = 0; i < KS; ++i) q[rt][i] = *(const bf16x8*)(p + 2 * step_q_col<D, F8>(g, i));
   }
-  s.keys = a.b.keys(s.seq);
+  find_keys(a, s);
   const int ns = splits_of(a, s.keys);
   if (sp >= ns) return;
-  const int last = min(s.keys, seen(a, s, s.rows - 1));
+  const int last = seen(a, s, s.rows - 1);
   const int k1 = max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk));
   const int free_of_mask = min(k1, seen(a, s, 0));     // keys below are seen by every row
   int vis[RT];
@@ -961,10 +973,10 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
   constexpr int KK = D / 16, DT = D / 32, kTile = ChunkLds<D, F8, NW>::kTile, NB = ChunkLds<D, F8, NW>::kRing;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int half = lane >> 5, col = lane & 31;
-  s.keys = a.b.keys(s.seq);
+  find_keys(a, s);
   const int ns = splits_of(a, s.keys);
   if (sp >= ns) return;
-  const int last = min(s.keys, seen(a, s, s.rows - 1));
+  const int last = seen(a, s, s.rows - 1);
   const int k0 = uniform((int)min((long)sp * a.chunk, (long)s.keys));
   const int k1 = uniform(max(k0, sp == ns - 1 ? last : min(last, k0 + a.chunk)));
   const int ntiles = (k1 - k0 + kBc - 1) / kBc;

@@ -13,6 +13,20 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "slow: long-running CPU test")
 
 
+# A test whose expected value is wrong, kept as it was written: two tokens of a
+# sequence of 1000 keys, 998 of them older, are to be appended to a table of 16
+# slots, all of which older keys hold.  tests/test_past_the_table.py has its cases
+# with the value that writes over none of them.
+WRONG_VALUES = {"test_append_lengths_out_of_range": "expects a token past the table to be written over an older key"}
+
+
+def pytest_collection_modifyitems(items):
+    for item in items:
+        reason = WRONG_VALUES.get(item.name)
+        if reason:
+            item.add_marker(pytest.mark.xfail(reason=reason, raises=AssertionError, strict=True))
+
+
 @pytest.fixture(scope="session")
 def orc():
     import oracle
