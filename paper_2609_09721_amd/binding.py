@@ -178,6 +178,23 @@ def _scratch(nbytes: int, stream=None) -> Optional[torch.Tensor]:
         return torch.empty(nbytes, dtype=torch.uint8, device="cuda")
 
 
+def _output(shape, dtype, device, stream=None) -> torch.Tensor:
+    """An output that the caller did not bring, in the memory pool of the stream
+    the call runs on: a block of the current stream's may be one that its queued
+    work still uses.  It is kept, once dropped, until the current stream is
+    done with it too, where its reader is most likely to be."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):        # a handle
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        out = torch.empty(shape, dtype=dtype, device=device)
+    now = torch.cuda.current_stream()
+    if now != stream:
+        out.record_stream(now)
+    return out
+
+
 def _splits(causal, kind) -> bool:
     """Whether calls of this form may run split over the keys at all."""
     return not causal and kind != PGEN_NOOP
@@ -519,12 +536,12 @@ def rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, axis: Optio
     dtype = x.dtype
     if dtype not in _DTYPES:
         raise ValueError("x must be bf16 or fp32")
-    if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=x.device)
-    elif out.shape != x.shape:
-        raise ValueError("out must have the shape of x")
     if not x.is_cuda:
         raise ValueError("x must be a CUDA tensor")
+    if out is None:
+        out = _output(x.shape, dtype, x.device, stream)
+    elif out.shape != x.shape:
+        raise ValueError("out must have the shape of x")
     dev = torch.cuda.current_device()
     xs = _tokens(x)
     xr, yr = _rows(xs, "x", dtype, dev), _rows(_tokens(out), "out", dtype, dev)
@@ -635,7 +652,7 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, batch: PagedB
         qr = _rows(q, "q", bf16, dev, None, D, T)
         heads = q.shape[1]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=bf16, device=q.device)
+            q_out = _output(q.shape, bf16, q.device, stream)
         orow = _rows(q_out, "q_out", bf16, dev, heads, D, T)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -659,7 +676,7 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, batch: PagedBatch, scale: Opt
     qr = _rows(q, "q", torch.bfloat16, dev, None, cache.head_dim)
     T, H, D = q.shape
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _output(q.shape, torch.float32, q.device, stream)
     dtype = _DTYPES.get(out.dtype)
     if dtype is None:
         raise ValueError("out must be bf16 or fp32")
