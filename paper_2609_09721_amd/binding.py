@@ -183,15 +183,14 @@ def _output(shape, dtype, device, stream=None) -> torch.Tensor:
     the call runs on: a block of the current stream's may be one that its queued
     work still uses.  It is kept, once dropped, until the current stream is
     done with it too, where its reader is most likely to be."""
-    if stream is None:
+    if stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()):
         return torch.empty(shape, dtype=dtype, device=device)
+    now = torch.cuda.current_stream()
     if not isinstance(stream, torch.cuda.Stream):        # a handle
         stream = torch.cuda.ExternalStream(stream.cuda_stream)
     with torch.cuda.stream(stream):
         out = torch.empty(shape, dtype=dtype, device=device)
-    now = torch.cuda.current_stream()
-    if now != stream:
-        out.record_stream(now)
+    out.record_stream(now)
     return out
 
 
@@ -243,7 +242,7 @@ def quant_v(v: torch.Tensor, seq_q: int = 1, heads_q: Optional[int] = None,
     sh = Shape(B, seq_q, S, heads_q or H, H, D)
     n = vhat_bytes(sh)
     if out is None:
-        out = torch.empty(n, dtype=torch.uint8, device=v.device)
+        out = _output(n, torch.uint8, v.device, stream)
     _check(lib().efq_quant_v_mxfp4(_ptr(v), ctypes.byref(sh), _ptr(out), out.numel(),
                                    _stream(stream)))
     return out
@@ -258,7 +257,7 @@ def attn_fwd_vhat(q, k, vhat, scale: Optional[float] = None, causal: bool = Fals
     if scale is None:
         scale = q.shape[-1] ** -0.5
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _output(q.shape, torch.float32, q.device, stream)
     ws, ws_n = _split_scratch(sh, causal, kind, False, stream)
     _check(lib().efq_attn_fwd_vhat_ws(_ptr(q), _ptr(k), _ptr(vhat), vhat.numel(), float(scale),
                                       int(causal), kind, _params(kind, params), _ptr(out),
@@ -278,7 +277,7 @@ def attn_fwd(q, k, v, scale: Optional[float] = None, causal: bool = False, kind=
     if scale is None:
         scale = q.shape[-1] ** -0.5
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _output(q.shape, torch.float32, q.device, stream)
     ws, ws_n = _workspace(sh, causal, kind, False, workspace, stream)
     _check(lib().efq_attn_fwd_ex(_ptr(q), _ptr(k), _ptr(v), float(scale), int(causal), kind,
                                  _params(kind, params), _ptr(out), ctypes.byref(sh), _ptr(ws), ws_n,
@@ -307,7 +306,7 @@ def efq_attn_fwd(q, k, v, scale=None, causal=False, out=None, stream=None):
     """The method's entry point: EFQ-Softmax, Mean operating point."""
     sh = shape_of(q, k)
     scale = q.shape[-1] ** -0.5 if scale is None else scale
-    out = torch.empty(q.shape, dtype=torch.float32, device=q.device) if out is None else out
+    out = _output(q.shape, torch.float32, q.device, stream) if out is None else out
     ws, ws_n = _workspace(sh, causal, PGEN_EFQ, False, None, stream)
     _check(lib().efq_attn_fwd_ex(_ptr(q), _ptr(k), _ptr(v), float(scale), int(causal), PGEN_EFQ,
                                  Params(*PARAMS_MEAN), _ptr(out), ctypes.byref(sh), _ptr(ws), ws_n,
@@ -319,7 +318,7 @@ def efq_attn_fwd_expq(q, k, v, scale=None, causal=False, out=None, stream=None):
     """The exp-then-quantize MXFP4 baseline."""
     sh = shape_of(q, k)
     scale = q.shape[-1] ** -0.5 if scale is None else scale
-    out = torch.empty(q.shape, dtype=torch.float32, device=q.device) if out is None else out
+    out = _output(q.shape, torch.float32, q.device, stream) if out is None else out
     ws, ws_n = _workspace(sh, causal, PGEN_EXPQ, False, None, stream)
     _check(lib().efq_attn_fwd_ex(_ptr(q), _ptr(k), _ptr(v), float(scale), int(causal), PGEN_EXPQ,
                                  Params(*PARAMS_MEAN), _ptr(out), ctypes.byref(sh), _ptr(ws), ws_n,
@@ -336,11 +335,11 @@ def attn_fwd_dump(q, k, vhat, scale=None, causal=False, kind="efq", params=None,
     Sk = k.shape[1]
     nblk = (Sk + 31) // 32
     dev = q.device
-    out = torch.empty(q.shape, dtype=torch.float32, device=dev)
-    codes = torch.empty((B, Hq, Sq, nblk * 16), dtype=torch.uint8, device=dev)
-    e8 = torch.empty((B, Hq, Sq, nblk), dtype=torch.uint8, device=dev)
-    row_m = torch.empty((B, Hq, Sq), dtype=torch.float32, device=dev)
-    row_l = torch.empty((B, Hq, Sq), dtype=torch.float32, device=dev)
+    out = _output(q.shape, torch.float32, dev, stream)
+    codes = _output((B, Hq, Sq, nblk * 16), torch.uint8, dev, stream)
+    e8 = _output((B, Hq, Sq, nblk), torch.uint8, dev, stream)
+    row_m = _output((B, Hq, Sq), torch.float32, dev, stream)
+    row_l = _output((B, Hq, Sq), torch.float32, dev, stream)
     _check(lib().efq_attn_fwd_dump(_ptr(q), _ptr(k), _ptr(vhat), vhat.numel(), float(scale),
                                    int(causal), kind, _params(kind, params), _ptr(out),
                                    ctypes.byref(sh), _ptr(codes), _ptr(e8), _ptr(row_m),
@@ -354,8 +353,8 @@ def quant_qk(q, k, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     _bf16(q, "q")
     _bf16(k, "k")
     sh = shape_of(q, k)
-    qh = torch.empty(int(lib().efq_qhat_bytes(ctypes.byref(sh))), dtype=torch.uint8, device=q.device)
-    kh = torch.empty(int(lib().efq_khat_bytes(ctypes.byref(sh))), dtype=torch.uint8, device=q.device)
+    qh = _output(int(lib().efq_qhat_bytes(ctypes.byref(sh))), torch.uint8, q.device, stream)
+    kh = _output(int(lib().efq_khat_bytes(ctypes.byref(sh))), torch.uint8, q.device, stream)
     _check(lib().efq_quant_qk_mxfp8(_ptr(q), _ptr(k), ctypes.byref(sh), _ptr(qh), qh.numel(),
                                     _ptr(kh), kh.numel(), _stream(stream)))
     return qh, kh
@@ -369,8 +368,7 @@ def attn_fwd_qk8(qhat, khat, vhat, shape: Shape, scale: Optional[float] = None,
     if scale is None:
         scale = shape.head_dim ** -0.5
     if out is None:
-        out = torch.empty((shape.batch, shape.seq_q, shape.heads_q, shape.head_dim),
-                          dtype=torch.float32, device=qhat.device)
+        out = _output((shape.batch, shape.seq_q, shape.heads_q, shape.head_dim), torch.float32, qhat.device, stream)
     ws, ws_n = _split_scratch(shape, causal, kind, True, stream)
     _check(lib().efq_attn_fwd_qk8_ws(_ptr(qhat), qhat.numel(), _ptr(khat), khat.numel(), _ptr(vhat),
                                      vhat.numel(), float(scale), int(causal), kind,
@@ -387,11 +385,11 @@ def attn_fwd_qk8_dump(qhat, khat, vhat, shape: Shape, scale=None, causal=False, 
     B, Sq, Hq, D, Sk = shape.batch, shape.seq_q, shape.heads_q, shape.head_dim, shape.seq_k
     nblk = (Sk + 31) // 32
     dev = qhat.device
-    out = torch.empty((B, Sq, Hq, D), dtype=torch.float32, device=dev)
-    codes = torch.empty((B, Hq, Sq, nblk * 16), dtype=torch.uint8, device=dev)
-    e8 = torch.empty((B, Hq, Sq, nblk), dtype=torch.uint8, device=dev)
-    row_m = torch.empty((B, Hq, Sq), dtype=torch.float32, device=dev)
-    row_l = torch.empty((B, Hq, Sq), dtype=torch.float32, device=dev)
+    out = _output((B, Sq, Hq, D), torch.float32, dev, stream)
+    codes = _output((B, Hq, Sq, nblk * 16), torch.uint8, dev, stream)
+    e8 = _output((B, Hq, Sq, nblk), torch.uint8, dev, stream)
+    row_m = _output((B, Hq, Sq), torch.float32, dev, stream)
+    row_l = _output((B, Hq, Sq), torch.float32, dev, stream)
     _check(lib().efq_attn_fwd_qk8_dump(_ptr(qhat), qhat.numel(), _ptr(khat), khat.numel(),
                                        _ptr(vhat), vhat.numel(), float(scale), int(causal), kind,
                                        _params(kind, params), _ptr(out), ctypes.byref(shape),
@@ -414,7 +412,7 @@ def attn_fwd_lowbit(q, k, v, scale: Optional[float] = None, causal: bool = False
     if scale is None:
         scale = q.shape[-1] ** -0.5
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = _output(q.shape, torch.float32, q.device, stream)
     ws, ws_n = _workspace(sh, causal, kind, True, workspace, stream)
     _check(lib().efq_attn_fwd_lowbit_ex(_ptr(q), _ptr(k), _ptr(v), float(scale), int(causal), kind,
                                         _params(kind, params), _ptr(out), ctypes.byref(sh), _ptr(ws),
@@ -455,7 +453,7 @@ def calibrate(q, k, v, o_ref, taus, hs, scale: Optional[float] = None, causal: b
     rho = np.zeros((len(ta), len(ha)), np.float64)
     best = Params(0.0, 0.0)
     nbytes = lib().efq_calibrate_workspace_bytes(ctypes.byref(sh), len(ta) * len(ha))
-    ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=q.device)
+    ws = _output(nbytes + 256, torch.uint8, q.device, stream)
     off = (-ws.data_ptr()) % 256
     _check(lib().efq_calibrate(_ptr(q), _ptr(k), _ptr(v), float(scale), int(causal), _ptr(o_ref),
                                ctypes.byref(sh), ta.ctypes.data_as(ctypes.c_void_p), len(ta),
@@ -707,8 +705,8 @@ def pgen(x: torch.Tensor, kind="efq", params=None, stream=None) -> Tuple[torch.T
         raise ValueError("x must be a contiguous 2-D fp32 CUDA tensor")
     rows, cols = x.shape
     kind = _kind(kind)
-    codes = torch.empty((rows, (cols + 1) // 2), dtype=torch.uint8, device=x.device)
-    e8 = torch.empty((rows, (cols + 31) // 32), dtype=torch.uint8, device=x.device)
+    codes = _output((rows, (cols + 1) // 2), torch.uint8, x.device, stream)
+    e8 = _output((rows, (cols + 31) // 32), torch.uint8, x.device, stream)
     _check(lib().efq_pgen(_ptr(x), rows, cols, kind, _params(kind, params), _ptr(codes), _ptr(e8),
                           _stream(stream)))
     return codes, e8
@@ -718,7 +716,7 @@ def pgen_bench(kind="efq", params=None, waves: int = 4096, iters: int = 256,
                checksum: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     kind = _kind(kind)
     if checksum is None:
-        checksum = torch.empty(waves, dtype=torch.int32, device="cuda")
+        checksum = _output(waves, torch.int32, "cuda", stream)
     _check(lib().efq_pgen_bench(kind, _params(kind, params), int(waves), int(iters),
                                 _ptr(checksum), _stream(stream)))
     return checksum
@@ -730,7 +728,7 @@ def clock_probe(blocks: int = 256, iters: int = 4000, out: Optional[torch.Tensor
     clock) and the s_memrealtime ticks (100 MHz) of an MFMA stream (the
     clock in GHz is 0.1 * col0 / col1); asynchronous on `stream`."""
     if out is None:
-        out = torch.empty((blocks, 2), dtype=torch.int64, device="cuda")
+        out = _output((blocks, 2), torch.int64, "cuda", stream)
     if out.dtype != torch.int64 or not out.is_cuda or out.numel() < 2 * blocks or not out.is_contiguous():
         raise ValueError("out must be a contiguous int64 CUDA tensor of at least 2 * blocks elements")
     _check(lib().efq_clock_probe(int(blocks), int(iters), _ptr(out), _stream(stream)))

@@ -52,7 +52,7 @@ def B(monkeypatch):
 
     class Library:
         def __getattr__(self, name):
-            return lambda *a: log.append((name, None)) or 0
+            return lambda *a: log.append((name, None)) or (256 if name.endswith("_bytes") and "paged" not in name else 0)
 
     monkeypatch.setattr(torch, "empty", empty)
     monkeypatch.setattr(torch.cuda, "stream", on)
@@ -90,13 +90,35 @@ def calls(B):
     yield "attn_paged", lambda **k: B.attn_paged(q, cache, batch, **k)
 
 
-NAMES = ["rope", "rope_bwd", "kv_append", "attn_paged"]
+def forward_calls(B):
+    """The attention forward's functions, those of their kinds that allocate."""
+    q, k = gpu(B, (1, 5, 4, 64)), gpu(B, (1, 5, 2, 64))
+    sh, buf, f32 = B.Shape(1, 5, 5, 4, 2, 64), gpu(B, (64,), torch.uint8), gpu(B, (1, 5, 4, 64), torch.float32)
+    yield "quant_v", lambda **a: B.quant_v(k, **a)
+    yield "quant_qk", lambda **a: B.quant_qk(q, k, **a)
+    yield "attn_fwd", lambda **a: B.attn_fwd(q, k, k, **a)
+    yield "attn_fwd_vhat", lambda **a: B.attn_fwd_vhat(q, k, buf, **a)
+    yield "efq_attn_fwd", lambda **a: B.efq_attn_fwd(q, k, k, **a)
+    yield "efq_attn_fwd_expq", lambda **a: B.efq_attn_fwd_expq(q, k, k, **a)
+    yield "attn_fwd_dump", lambda **a: B.attn_fwd_dump(q, k, buf, **a)
+    yield "attn_fwd_qk8", lambda **a: B.attn_fwd_qk8(buf, buf, buf, sh, **a)
+    yield "attn_fwd_qk8_dump", lambda **a: B.attn_fwd_qk8_dump(buf, buf, buf, sh, **a)
+    yield "attn_fwd_lowbit", lambda **a: B.attn_fwd_lowbit(q, k, k, **a)
+    yield "calibrate", lambda **a: B.calibrate(q, k, k, f32, [-3.0], [2.0], **a)
+    yield "pgen", lambda **a: B.pgen(gpu(B, (2, 64), torch.float32), **a)
+    yield "pgen_bench", lambda **a: B.pgen_bench(**a)
+    yield "clock_probe", lambda **a: B.clock_probe(**a)
+
+
+NAMES = ["rope", "rope_bwd", "kv_append", "attn_paged", "quant_v", "quant_qk", "attn_fwd", "attn_fwd_vhat", "efq_attn_fwd",
+         "efq_attn_fwd_expq", "attn_fwd_dump", "attn_fwd_qk8", "attn_fwd_qk8_dump", "attn_fwd_lowbit", "calibrate", "pgen",
+         "pgen_bench", "clock_probe"]
 
 
 @pytest.mark.parametrize("name", NAMES)
 def test_outputs_are_in_the_pool_of_the_calls_stream(B, name):
-    f = dict(calls(B))[name]
-    for stream, pool, kept in ((None, None, False), (SIDE, SIDE, True), (CURRENT, CURRENT, False), (Handle(), WRAPPED, True)):
+    f = {**dict(calls(B)), **dict(forward_calls(B))}[name]
+    for stream, pool, kept in ((None, None, False), (SIDE, SIDE, True), (CURRENT, None, False), (Handle(), WRAPPED, True)):
         del B.log[:]
         f(stream=stream)
         outputs = [x for x in B.log if x[0] == "allocated"]
