@@ -397,8 +397,9 @@ int efq_kv_append(const efq_rows *k, const efq_rows *v, const efq_cache *cache, 
  * out_dtype EFQ_BF16 or EFQ_F32.  lse (fp32 [tokens][heads_q], may be NULL)
  * receives log sum exp of the scaled scores.  A token that sees no key gets 0
  * and -inf.  Scores, sums and accumulators are fp32, the exponential is not
- * quantised; the probabilities enter the second product in bf16, relative
- * to the row's maximum.  What the cache holds outside the sequences (unused
+ * quantised; the probabilities enter the second product rounded to bf16 (each off
+ * by at most 2^-8 of itself, of which a row that one key dominates sees nothing);
+ * lse is of the unrounded ones.  What the cache holds outside the sequences (unused
  * slots and pages) may be anything; queries, and keys and values of the
  * sequences, must be finite, scores within 2^30 (an fp32 score has no digit left
  * for the exponential there) and values within 2^80 (sums are not normalised

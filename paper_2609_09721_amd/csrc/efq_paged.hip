@@ -28,6 +28,7 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
   const f32x2 x = {lo, hi};
   return __builtin_bit_cast(unsigned, __builtin_convertvector(x, bf16x2));
 }
+constexpr unsigned kOnes = 0x3f803f80u;    // a pair of ones
 __device__ __forceinline__ float bf16_lo(unsigned u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(unsigned u) { return __uint_as_float(u & 0xffff0000u); }
 
@@ -411,8 +412,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 // the transposing read (ds_read_b64_tr_b16: 16 lanes give 4 rows x 16 columns,
 // each gets one column's 4 values).  The running maximum is kept in log2 units
 // (score scale log2 e), in which alpha and the probabilities are one fma and
-// one exp2; the row sum is that of the fp32 probabilities, the product takes
-// them rounded to bf16 (at most 2^-8 of each, independent of one another).
+// one exp2.  The row sum is that of the fp32 probabilities, the product takes them
+// rounded to bf16 (at most 2^-8 of each, independent of one another), and a row
+// that one key dominates is still exact: in the step kernel its probability is 1, in
+// the chunk kernel O is divided by the sum of the rounded ones.
 struct PagedArgs {
   const char* q;
   char* out;
@@ -963,8 +966,18 @@ struct ChunkFeed {
 // The running reference of a row need not be its maximum: it moves only when a
 // lane's probabilities of a tile sum up to more than this, so almost never
 // after the first tile, and until then no maximum is taken and nothing rescaled.
-// It costs no precision (the probabilities' rounding is relative, the sums are
-// fp32: 2^16 a tile and lane, so below 2^42 in all, times the values).
+// The sums stay below 2^42 (2^16 a tile and lane), times the values.  With the
+// maximum as the reference a dominant key's probability would be 1 and exact; here
+// it is rounded like any other, so O is divided by the sum of the rounded ones, in
+// which a dominant key's rounding cancels (the matrix core sums them, from the
+// product's own operand), while log-sum-exp and the weights of a row's parts keep
+// the unrounded sum.  Relative error of O in fp32, by the unrounded sum / the rounded
+// one / with the maximum as the reference: 2048 tokens behind 14000 (D 128, bf16)
+// 0.00164 / 0.00150 / 0.00099, 4096 behind 28000 (MXFP8) 0.00162 / 0.00119 / 0.00068,
+// up to 1500 behind 3001 (D 64) 0.00163 / 0.00125 / 0.00078; it costs 2 to 4 % of a
+// call (431 to 445 us, 1670 to 1715, 81 to 83), the maximum 30 to 50 %.  A limit of 64
+// without it: 0.00142, 0.00124 and 0.00138 for 441, 1686 and 85 us, and up to 9 % on
+// short rows (300 tokens 16.6 to 18.2 us).
 constexpr float kMostSum = 65536.0f;
 
 // One slot's rows, split sp of their keys.
@@ -1054,6 +1067,13 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
 
   f32x16 sc[2];
   bf16x8 p[4];
+  // The sums of rounded probabilities, the same in all four: the 16-wide product
+  // takes a P operand's lanes l + 16 for k 8 to 15, 24 to 31 of column l % 16, so rows
+  // 0 to 3 and 8 to 11 of its result, which lanes 0 to 15 and 32 to 47 get, sum the
+  // other k, and the rest those.
+  f32x4 lr = {0.0f, 0.0f, 0.0f, 0.0f};
+  const unsigned own = ((lane >> 4) & 1) == ((lane >> 2) & 1) ? kOnes : 0u;
+  const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{own, own, own, own});
   // M(j) is NV products of V tile j with its probabilities, then NK of K tile
   // j + 1 with Q, in pairs whose second operand is read first, so that one wait
   // serves both.  Operands are read kAhead products before they are used (an LDS
@@ -1097,6 +1117,7 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
       __builtin_amdgcn_sched_barrier(0);
       product(std::integral_constant<int, N>{});
       read_op(slot, std::integral_constant<int, N + kAhead + 1>{});
+      if constexpr (N < NV && N % DT == 0) lr = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[N / DT], lr, 0, 0, 0);
       // the step's loads, in the products' shadow
       if constexpr (N % kEvery == kEvery / 2) fetch_one(slot, std::integral_constant<int, N / kEvery>{}, j + NB);
       __builtin_amdgcn_sched_barrier(0);
@@ -1144,6 +1165,7 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
       m = mn;
       ref = mn == -INFINITY ? 0.0f : mn;
       l *= alpha;
+      lr *= alpha;
 #pragma unroll
       for (int i = 0; i < DT; ++i) o[i] *= alpha;
       probabilities();
@@ -1204,7 +1226,7 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
   if (r >= s.rows) return;
   const long at = (long)tok * a.Hq + hq;
   if (ns == 1) {
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l > 0.0f ? 1.0f / lr[0] : 0.0f;
     char* p = a.out + tok * a.o_token + hq * a.o_head;
 #pragma unroll
     for (int i = 0; i < DT; ++i)
@@ -1216,11 +1238,13 @@ __device__ __forceinline__ void chunk_rows(const PagedArgs& a, Slot& s, int h, i
     if (half == 0 && a.lse) a.lse[at] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : -INFINITY;
   } else {
     float* p = a.part_o + ((long)sp * a.rows + at) * D;
+    const float weight = l > 0.0f ? l / lr[0] : 0.0f;      // to that of the unrounded sum
 #pragma unroll
     for (int i = 0; i < DT; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        *(f32x4*)(p + 32 * i + 8 * j + 4 * half) = f32x4{o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]};
+        *(f32x4*)(p + 32 * i + 8 * j + 4 * half) =
+            f32x4{o[i][4 * j] * weight, o[i][4 * j + 1] * weight, o[i][4 * j + 2] * weight, o[i][4 * j + 3] * weight};
     if (half == 0) a.part_ml[(long)sp * a.rows + at] = make_float2(m, l);
   }
 }
