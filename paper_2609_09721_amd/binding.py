@@ -530,16 +530,29 @@ def rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, axis: Optio
 
     pos: int32 [axes, tokens] (or [tokens]); inv_freq: fp32 [pairs]; axis: int32
     [pairs], None with one axis.  interleaved: pairs of neighbours instead of
-    halves.  Values behind 2 * pairs pass.  out may be x."""
+    halves.  Values behind 2 * pairs pass.  out may be x.
+
+    Differentiable in x (any number of times): the gradient is the turn back, run
+    on the stream that is current in the backward pass.  With out no gradient can
+    be recorded, and the frequencies have none."""
     dtype = x.dtype
     if dtype not in _DTYPES:
         raise ValueError("x must be bf16 or fp32")
     if not x.is_cuda:
         raise ValueError("x must be a CUDA tensor")
+    if (x.requires_grad or inv_freq.requires_grad) and torch.is_grad_enabled():
+        if inv_freq.requires_grad:
+            raise ValueError("inv_freq requires a gradient, which rope does not have")
+        if out is not None:
+            raise ValueError("out cannot be given where x requires a gradient")
+        return _Turn.apply(x, pos, inv_freq, axis, interleaved, stream, _inverse)
     if out is None:
         out = _output(x.shape, dtype, x.device, stream)
-    elif out.shape != x.shape:
-        raise ValueError("out must have the shape of x")
+    else:
+        if out.shape != x.shape:
+            raise ValueError("out must have the shape of x")
+        if not out.is_inference():
+            torch.autograd.graph.increment_version(out)     # what recorded out's old values must not use the new ones
     dev = torch.cuda.current_device()
     xs = _tokens(x)
     xr, yr = _rows(xs, "x", dtype, dev), _rows(_tokens(out), "out", dtype, dev)
@@ -547,6 +560,23 @@ def rope(x: torch.Tensor, pos: torch.Tensor, inv_freq: torch.Tensor, axis: Optio
     rot = _rotary(pos, inv_freq, axis, interleaved, T, dev)
     _check(lib().efq_rope(xr, yr, T, H, D, _DTYPES[dtype], rot, _inverse, _stream(stream)))
     return out
+
+
+class _Turn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, pos, inv_freq, axis, interleaved, stream, inverse):
+        ctx.save_for_backward(pos, inv_freq, axis)
+        ctx.turn = interleaved, 1 - inverse
+        return rope(x, pos, inv_freq, axis, interleaved, None, stream, inverse)
+
+    @staticmethod
+    def backward(ctx, grad):
+        interleaved, inverse = ctx.turn
+        grad = grad.contiguous()            # a gradient may be a broadcast one, or not aligned as rows are
+        if grad.data_ptr() % 16:
+            grad = grad.clone()
+        back = rope(grad, *ctx.saved_tensors, interleaved, _inverse=inverse)
+        return back, None, None, None, None, None, None
 
 
 def rope_bwd(grad, pos, inv_freq, axis=None, interleaved=False, out=None, stream=None):
@@ -633,7 +663,7 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, cache: PagedCache, batch: PagedB
               inv_freq: Optional[torch.Tensor] = None, axis: Optional[torch.Tensor] = None, interleaved: bool = False,
               stream=None) -> Optional[torch.Tensor]:
     """New keys and values (bf16 [tokens, heads_kv, head_dim], any strides) into
-    the cache's pages, the keys with their positions applied when pos and
+    the cache's pages (no gradient passes a cache), the keys with their positions applied when pos and
     inv_freq are given (as in rope).  With q its rows are turned too, into q_out
     (new when None; may be q), which is returned."""
     dev = _together(cache, batch)
@@ -669,7 +699,7 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, batch: PagedBatch, scale: Opt
     any strides) over the pages of their sequences; a token sees the keys up to
     its own (causal) or all.  out: bf16 or fp32 of q's shape (fp32 when None);
     lse: fp32 [tokens, heads_q] receives the log-sum-exp.  Padding tokens keep
-    what out and lse held."""
+    what out and lse held.  For inference: no gradient is recorded."""
     dev = _together(cache, batch)
     qr = _rows(q, "q", torch.bfloat16, dev, None, cache.head_dim)
     T, H, D = q.shape
