@@ -156,7 +156,7 @@ __device__ __forceinline__ void turn_halves(Piece<F32>& lo, Piece<F32>& hi, cons
   }
 }
 
-constexpr int kMostShared = 4;     // most tokens of a workgroup
+constexpr int kMostShared = 8;     // most tokens of a workgroup
 
 // An item is a 16-byte piece of a head (neighbouring pairs) or the two pieces of
 // the same pairs (halves), so that the lanes of a load lie side by side; pieces
@@ -214,7 +214,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
 
 // ------------------------------------------------------------ paged batch
 constexpr int kMostKeys = 1 << 30;         // of a sequence: key indexes stay in 32 bits
-constexpr int kMostTokens = 1 << 26;       // of a call: launches stay within 2^32 threads
+constexpr int kMostTokens = 1 << 26;       // of a call
+constexpr long kMostGroups = 0xffffffffL / 256;   // of a launch: its threads are counted in 32 bits
 struct Batch {
   const int32_t *q_start, *seq_k, *table;
   int seqs, tokens, width, pages, shift;   // page_size = 1 << shift
@@ -1406,9 +1407,12 @@ Batch batch_args(const efq_batch* b, const efq_cache* c) {
 // tokens of 768 pieces (fp32) at 1 / 2 / 4 / 8 tokens 139 / 149 / 156 / 163 us, 8192 of 640 (bf16)
 // 30.7 / 30.6 / 32.2, 20000 of 128 23.8 / 19.2 / 16.8 / 18.0.  Append, whose pages hold
 // a head's tokens side by side: 11400 tokens (32/8 heads, D 128) into MXFP8 pages at
-// 1 / 2 / 4 / 8 tokens 71 / 64 / 61 / 65 us.
+// 1 / 2 / 4 / 8 tokens 71 / 64 / 61 / 65 us.  More tokens than a launch has workgroups
+// for share them, up to kMostShared.
 void token_grid(int tokens, int threads_per_token, int enough, int& tt, int& parts) {
-  for (tt = kMostShared; tt > 1 && (tokens < tt * 8 * kCUs || tt / 2 * threads_per_token >= enough); tt /= 2) {}
+  static_assert((kMostTokens + kMostShared - 1) / kMostShared <= kMostGroups, "the most tokens fit a launch");
+  for (tt = 4; tt > 1 && (tokens < tt * 8 * kCUs || tt / 2 * threads_per_token >= enough); tt /= 2) {}
+  while (((long)tokens + tt - 1) / tt > kMostGroups) tt *= 2;
   parts = tt > 1 || tokens > 4 * kCUs ? 1 : (threads_per_token + 255) / 256;
 }
 
