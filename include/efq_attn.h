@@ -394,7 +394,8 @@ int efq_kv_append(const efq_rows *k, const efq_rows *v, const efq_cache *cache, 
  * causal != 0: a token sees the keys up to its own (token j of n new ones of a
  * sequence with s keys sees s - n + j + 1); otherwise all s.  q bf16
  * [tokens][heads_q][head_dim], heads_q a multiple of heads_kv; out likewise,
- * out_dtype EFQ_BF16 or EFQ_F32.  lse (fp32 [tokens][heads_q], may be NULL)
+ * out_dtype EFQ_BF16 or EFQ_F32; a bf16 out may be q (in place, the strides alike),
+ * other overlaps are not supported.  lse (fp32 [tokens][heads_q], may be NULL)
  * receives log sum exp of the scaled scores.  A token that sees no key gets 0
  * and -inf.  Scores, sums and accumulators are fp32, the exponential is not
  * quantised; the probabilities enter the second product rounded to bf16 (each off

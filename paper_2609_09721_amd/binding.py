@@ -697,7 +697,8 @@ def attn_paged(q: torch.Tensor, cache: PagedCache, batch: PagedBatch, scale: Opt
                workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Softmax attention of the new tokens q (bf16 [tokens, heads_q, head_dim],
     any strides) over the pages of their sequences; a token sees the keys up to
-    its own (causal) or all.  out: bf16 or fp32 of q's shape (fp32 when None);
+    its own (causal) or all.  out: bf16 or fp32 of q's shape (fp32 when None; a
+    bf16 one may be q);
     lse: fp32 [tokens, heads_q] receives the log-sum-exp.  Padding tokens keep
     what out and lse held.  For inference: no gradient is recorded."""
     dev = _together(cache, batch)

@@ -1657,8 +1657,9 @@ int efq_attn_paged(const efq_rows* q, int heads_q, const efq_cache* cache, const
   if (batch->tokens == 0) return EFQ_OK;
   const int D = cache->head_dim;
   if ((rc = check_rows(q, "q", 2)) ||
-      (rc = check_out_rows(out, "out", out_dtype == EFQ_F32 ? 4 : 2, batch->tokens, heads_q, D)))
+      (rc = check_out_rows(out, "out", out_dtype == EFQ_F32 ? 4 : 2, batch->tokens, heads_q, D, q)))
     return rc;
+  if (out_dtype == EFQ_F32 && out->data == q->data) return fail(EFQ_EINVAL, "out: fp32 rows in the place of q's");
   if ((uintptr_t)lse & 3) return fail(EFQ_EINVAL, "lse must be 4-byte aligned");
   if (ws_bytes != 0 && !ws) return fail(EFQ_EWORKSPACE, "workspace is NULL");
   if (ws && !aligned16(ws)) return fail(EFQ_EINVAL, "workspace must be 16-byte aligned");
