@@ -160,3 +160,34 @@ def test_another_stream_with_outputs_of_its_own(handle):
             assert torch.equal(g, w)
         del got
         side.wait_stream(torch.cuda.current_stream())
+
+
+@pytest.mark.gpu
+def test_captured_on_a_forked_stream():
+    """Calls on a stream that a capture forks to, with outputs of their own; replays between eager calls."""
+    from paper_2609_09721_amd import binding as B
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()
+    x, kv = torch.zeros(40, 8, 64, device="cuda").bfloat16(), torch.zeros(40, 2, 64, device="cuda").bfloat16()
+    pos, inv = torch.arange(40, dtype=torch.int32).cuda(), torch.rand(32).cuda()
+    cache = B.PagedCache.empty(3, 16, 2, 64)
+    batch = B.PagedBatch(i32([0, 40]), i32([40]), i32([[2, 0, 1]]), max_q=40, max_k=40)
+    side = torch.cuda.Stream()
+
+    def step(**k):
+        q = B.kv_append(kv, kv, cache, batch, q=x, pos=pos, inv_freq=inv, **k)
+        return B.attn_paged(B.rope(q, pos, inv, **k), cache, batch, **k)
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = step(stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        x.copy_(torch.randn(x.shape)), kv.copy_(torch.randn(kv.shape))
+        graph.replay()
+        torch.cuda.synchronize()
+        now = got.clone()
+        assert torch.equal(now, step()), i
+        torch.cuda.synchronize()
