@@ -360,7 +360,8 @@ typedef struct efq_cache {
  * newest ones are the tokens q_start[i] .. q_start[i + 1] - 1 of the call, in
  * order.  Key t of sequence i lies in slot t % page_size of page
  * page_table[i][t / page_size].  Tokens from q_start[seqs] on are padding:
- * they are not appended, and their outputs stay as they were.
+ * they are not appended, and their outputs stay as they were.  At most 2^20
+ * sequences and 2^26 tokens.
  * tokens: rows of the call's tensors.  max_q, max_k: the largest number of new
  * tokens and of keys of a sequence as far as the host knows (0: unknown); they
  * choose how the work is split, so the order of sums, and wrong ones cost time,
@@ -405,6 +406,8 @@ int efq_kv_append(const efq_rows *k, const efq_rows *v, const efq_cache *cache, 
  * sequences, must be finite, scores within 2^30 (an fp32 score has no digit left
  * for the exponential there) and values within 2^80 (sums are not normalised
  * before the end).
+ * tokens * heads_q is below 2^25, and tokens * heads_q / 16 + seqs * heads_kv below
+ * 2^22 (EFQ_EUNSUPPORTED).
  * Work is split over the keys where the rows alone do not fill the chip, which
  * takes scratch memory: ws of efq_attn_paged_workspace_bytes (0 where nothing
  * is split), 16-byte aligned; without it (NULL, 0) or with less, the call runs

@@ -499,9 +499,11 @@ __device__ __forceinline__ void put4(char* at, int f32, f32x4 o) {
 // D 128, 128 KB a CU with its two workgroups.  16 RT rows: K in matrix-operand
 // order straight into registers, V through LDS for its transposition.
 //
-// One token over 131000 keys (32/8 heads, D 128, bf16; 537 MB) takes 84 us, 6.35
-// TB/s, where a kernel that only reads reaches 6.0 to 6.2; 17 sequences of 5000
-// to 20000 keys (797 MB) 138 us, 5.8 TB/s.
+// One token over 131000 keys (32/8 heads, D 128, bf16; 537 MB) takes 84 to 86 us, 6.2
+// to 6.4 TB/s, in caches that are a process's first allocations, and 97 to 110 us, 4.9
+// to 5.5 TB/s, in memory that was handed out before; a kernel that streams the same
+// bytes in order reaches 6.7 TB/s in both.  17 sequences of 5000 to 20000 keys (797
+// MB) 138 us, 5.8 TB/s.
 constexpr int kStepWaves = 4;
 constexpr int kStepHalves = 2;     // 16-key halves of a wave's tile
 
@@ -816,13 +818,15 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
 // too short for that (a barrier costs a tenth of it) and rows are short enough
 // for three workgroups of four waves a CU, which overlap by themselves.
 //
-// 2048 tokens behind 14000 keys (32/8 heads, D 128, bf16; 504 GFLOP) take 418
-// us, 1206 TFLOP/s; 4096 behind 28000, MXFP8, 1620 us, 1244.  The matrix core is
-// busy 63 % of the cycles and the chip lowers its clock to 1.77 GHz for the power
-// (on keys and values of one constant it runs at 2.23).  D 64, 7 sequences of up to
-// 1500 tokens behind 3001 (16/4 heads): 80 us, 718 TFLOP/s; its 16 exponentials and 8
-// matrix instructions a lane and tile half take 256 cycles each, and the vector
-// unit has sums, scaling and packing besides.
+// 2048 tokens behind 14000 keys (32/8 heads, D 128, bf16; 504 GFLOP) take 445 to 461
+// us by the box, 1094 to 1133 TFLOP/s; 4096 behind 28000, MXFP8, 1713 to 1764 us, 1143
+// to 1177.  The matrix core is busy 63 % of the cycles and the chip lowers its clock
+// for the power: 1.66 GHz in twenty calls in a row, which then take 492 us (on keys and
+// values of one constant it runs at 2.23).  D 64, 7 sequences of up to 1500 tokens
+// behind 3001 (16/4 heads): 82 to 85 us, 674 to 701 TFLOP/s.  There neither unit is
+// full (vector 0.45, matrix 0.33 of the cycles): 800 workgroups of 15 to 63 tiles go
+// to 768 places in the order of their slots, so the fullest CU has 137 tiles or more
+// where an even share is 111.
 template <int N, int I = 0, typename F>
 __device__ __forceinline__ void static_for(F&& f) {
   if constexpr (I < N) {
@@ -853,8 +857,9 @@ __device__ __forceinline__ int chunk_v_swz(int r) { return D == 128 ? ((r & 3) <
 // count it too, and so only wait longer.
 __device__ __forceinline__ void load_lds_1k(u32x4 rsrc, unsigned to, int voff) {
   // (five wait states from a vector instruction that writes a scalar register to
-  // a memory instruction that reads it, one from the write of m0, which the
-  // compiler sets anew before any instruction of its own that reads it)
+  // a memory instruction that reads it, one from the write of m0.  The compiler
+  // reserves m0: it keeps nothing there over instructions, so there is nothing to
+  // clobber, and these kernels have no other instruction that reads it)
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :: "s"(to), "v"(voff), "s"(rsrc) : "memory");
 }
