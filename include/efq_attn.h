@@ -399,13 +399,14 @@ int efq_kv_append(const efq_rows *k, const efq_rows *v, const efq_cache *cache, 
  * other overlaps are not supported.  lse (fp32 [tokens][heads_q], may be NULL)
  * receives log sum exp of the scaled scores.  A token that sees no key gets 0
  * and -inf.  Scores, sums and accumulators are fp32, the exponential is not
- * quantised; the probabilities enter the second product rounded to bf16 (each off
- * by at most 2^-8 of itself, of which a row that one key dominates sees nothing);
- * lse is of the unrounded ones.  What the cache holds outside the sequences (unused
- * slots and pages) may be anything; queries, and keys and values of the
- * sequences, must be finite, scores within 2^30 (an fp32 score has no digit left
- * for the exponential there) and values within 2^80 (sums are not normalised
- * before the end).
+ * quantised.  Where sequences have a few tokens (max_q * heads_q / heads_kv up to
+ * 32, 64 with MXFP8 pages or 64-wide heads) the second product takes each
+ * probability to 2^-16 of itself; where they have more, rounded to bf16 (2^-8, of
+ * which a row that one key dominates sees nothing).  lse is of the unrounded ones.
+ * What the cache holds outside the sequences (unused slots and pages) may be
+ * anything; queries, and keys and values of the sequences, must be finite, scores
+ * within 2^30 (an fp32 score has no digit left for the exponential there) and
+ * values within 2^80 (sums are not normalised before the end).
  * tokens * heads_q is below 2^25, and tokens * heads_q / 16 + seqs * heads_kv below
  * 2^22 (EFQ_EUNSUPPORTED).
  * Work is split over the keys where the rows alone do not fill the chip, which
