@@ -830,8 +830,8 @@ __global__ __launch_bounds__(64 * kStepWaves, 2) void paged_step_kernel(PagedArg
 // 2048 tokens behind 14000 keys (32/8 heads, D 128, bf16; 504 GFLOP) take 445 to 461
 // us by the box, 1094 to 1133 TFLOP/s; 4096 behind 28000, MXFP8, 1713 to 1764 us, 1143
 // to 1177.  The matrix core is busy 63 % of the cycles and the chip lowers its clock
-// for the power: 1.66 GHz in twenty calls in a row, which then take 492 us (on keys and
-// values of one constant it runs at 2.23).  D 64, 7 sequences of up to 1500 tokens
+// for the power: 1.66 to 1.72 GHz in twenty calls in a row, which then take 475 to 492
+// us (on keys and values of one constant it runs at 2.23).  D 64, 7 sequences of up to 1500 tokens
 // behind 3001 (16/4 heads): 82 to 85 us, 674 to 701 TFLOP/s.  There neither unit is
 // full (vector 0.45, matrix 0.33 of the cycles): 800 workgroups of 15 to 63 tiles go
 // to 768 places in the order of their slots, so the fullest CU has 137 tiles or more
