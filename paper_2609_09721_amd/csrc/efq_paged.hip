@@ -1458,8 +1458,9 @@ PagedPlan paged_plan(const efq_cache* c, const efq_batch* b, int heads_q) {
   const long rows = most_q * G;
   // The chunk kernel's waves share what they read, the step kernel's rows all
   // pass through every wave.  32 rows: 16 sequences x 8 tokens over 4000 keys
-  // (32/8 heads, D 128, bf16) step 43 us, chunk 44; 64 rows: x 16 tokens 61 and
-  // 46, MXFP8 40 and 49; D 64, 4 sequences x 16 tokens 13.4 and 14.5.
+  // (32/8 heads, D 128, bf16) step 41 us, chunk 47; 64 rows: x 16 tokens 61 and
+  // 49, MXFP8 43 and 49 (one sequence over 20000 keys 29 and 27); D 64, 16 tokens over
+  // 20000 keys 17.0 and 18.2.
   const bool low = c->format == EFQ_CACHE_MXFP8, narrow = c->head_dim == 64;
   p.rt = rows <= 16 ? 1 : rows <= (low || narrow ? 64 : 32) ? 2 : 0;
   p.bm = p.rt ? 16 * p.rt : narrow ? 128 : 256;
